@@ -263,6 +263,96 @@ int sgprs_avgpool_fc_static(int dtype, int n, int hw, int cin, int cout, const v
                             const void *w, const float *bias, float *logits, sgprs_pool_t *pool,
                             int partition);
 
+/* ---------------------------------------------------- attention blocks ----
+ * The operators of an attention block on a channels-last feature map, or of a
+ * transformer layer, for networks that run beside the convolutional ones:
+ * token- or pixel-wise products, a norm whose statistics are the input's own,
+ * and attention.  Both dtypes; sums, statistics and softmax in fp32, results
+ * rounded once on store.
+ *
+ * Strides count elements; 0 stands for the dense value.  Rows may start at any
+ * multiple of the element size; where pointers are 16-byte aligned and strides
+ * multiples of 16 bytes, wider loads are used.  Strides up to 2^20 elements
+ * between rows: UNSUPPORTED beyond that.  A call of zero rows (m, n or total_q
+ * 0) succeeds and enqueues nothing.  Outputs must not overlap inputs unless the
+ * operator says so. */
+typedef enum {
+    SGPRS_ACT_NONE = 0,
+    SGPRS_ACT_RELU = 1, /* a NaN stays a NaN */
+    SGPRS_ACT_GELU = 2, /* z/2 (1 + erf(z / sqrt 2)) */
+    SGPRS_ACT_SILU = 3  /* z / (1 + exp(-z)) */
+} sgprs_act_t;
+
+/* y[i][j] = act( sum_k x[i][k] w[j][k] + bias[j] ) + residual[i][j], or, with
+ * residual_first, act( ... + residual ). */
+typedef struct {
+    int m, n, k;                    /* rows of x, outputs, inputs */
+    int dtype;                      /* sgprs_dtype_t of x, w, residual, y */
+    int act;                        /* sgprs_act_t */
+    int residual_first;             /* 1: the residual is added before the activation */
+    long long ldx, ldw, ldr, ldy;   /* between rows of x, w, residual, y; 0: k, k, n, n */
+} sgprs_linear_desc_t;
+/* Scratch needed on a partition of partition_cus CUs (0 where K is not split over workgroups). */
+int sgprs_linear_workspace(const sgprs_linear_desc_t *d, int partition_cus, size_t *bytes);
+/* x [m][k], w [n][k], residual NULL or [m][n], y [m][n] DEVICE in dtype; bias
+ * NULL or DEVICE fp32[n].  y may be the residual itself (same pointer and
+ * stride).  workspace: DEVICE, 16-byte aligned, at least
+ * sgprs_linear_workspace() bytes (may be NULL if 0). */
+int sgprs_linear(const sgprs_linear_desc_t *d, const void *x, const void *w, const float *bias,
+                 const void *residual, void *y, void *workspace, size_t workspace_bytes,
+                 sgprs_pool_t *pool, int partition);
+
+/* Group norm, channels last: the c channels of an image form `groups` groups of
+ * c / groups neighbours; mean and (biased) variance are those of a group over
+ * all hw positions, and
+ *   y = act( (x - mean) / sqrt(var + eps) * gamma[c] + beta[c] (+ residual) ).
+ * With hw = 1 and groups = 1 it is the layer norm of n tokens. */
+typedef struct {
+    int n, hw, c, groups;           /* c % groups == 0 */
+    int dtype;                      /* of x, residual, y */
+    int act;                        /* sgprs_act_t, of the sum with the residual */
+    float eps;                      /* >= 0 */
+    long long ldx, ldr, ldy;        /* between positions; 0: c.  An image starts hw positions behind the last */
+} sgprs_group_norm_desc_t;
+int sgprs_group_norm_workspace(const sgprs_group_norm_desc_t *d, int partition_cus, size_t *bytes);
+/* x, residual (may be NULL), y DEVICE in dtype; gamma, beta NULL (1, 0) or
+ * DEVICE fp32[c].  y may be x or the residual (same pointer and stride). */
+int sgprs_group_norm(const sgprs_group_norm_desc_t *d, const void *x, const float *gamma,
+                     const float *beta, const void *residual, void *y, void *workspace,
+                     size_t workspace_bytes, sgprs_pool_t *pool, int partition);
+
+/* Attention over n_seqs packed sequences: the queries of sequence s are tokens
+ * q_offsets[s] .. q_offsets[s+1]-1 of q, its keys and values tokens
+ * kv_offsets[s] .. kv_offsets[s+1]-1 of k and v, and query head h reads key
+ * head h / (heads / kv_heads):
+ *   o = sum_j p_j v_j,  p = softmax_j( scale * q . k_j )
+ * over the sequence's keys; causal: the queries are the sequence's last tokens,
+ * so query i of nq sees keys j <= i + nk - nq.  A query that sees no key gets
+ * zeros; what k and v hold at keys that a query does not see (NaN included)
+ * does not reach it.  One query per sequence against a cache is the case of
+ * max_q = 1. */
+typedef struct {
+    int n_seqs;
+    int total_q, total_kv;          /* tokens in q and o, in k and v */
+    int max_q, max_kv;              /* the longest sequence's */
+    int heads, kv_heads, head_dim;  /* heads % kv_heads == 0; head_dim a multiple of 8, up to 128 */
+    int dtype;                      /* of q, k, v, o */
+    int causal;
+    float scale;                    /* 0: 1 / sqrt(head_dim) */
+    long long ldq, ldk, ldv, ldo;   /* between tokens; 0: (kv_)heads * head_dim */
+    long long hq, hk, hv, ho;       /* between heads; 0: head_dim.  (tokens first or heads first) */
+} sgprs_attention_desc_t;
+int sgprs_attention_workspace(const sgprs_attention_desc_t *d, int partition_cus, size_t *bytes);
+/* q, k, v, o DEVICE, 16-byte aligned, strides multiples of 16 bytes.
+ * q_offsets, kv_offsets: DEVICE int32[n_seqs + 1], non-decreasing, from 0 to
+ * total_q and total_kv.  They are read by the kernels, so their values cannot
+ * be refused: with others, and with a sequence longer than max_q or max_kv
+ * says, which rows are written is unspecified, but nothing outside the tensors
+ * is read or written. */
+int sgprs_attention(const sgprs_attention_desc_t *d, const void *q, const void *k, const void *v,
+                    const int *q_offsets, const int *kv_offsets, void *o, void *workspace,
+                    size_t workspace_bytes, sgprs_pool_t *pool, int partition);
+
 /* ------------------------------------------------------------------ task --
  * Task tau_i = one ResNet18 instance, split into the paper's six stages:
  *   0 conv7x7/2+BN+ReLU+maxpool3x3/2, 1..4 layer1..layer4 (two BasicBlocks

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import (POINTER, c_char_p, c_double, c_float, c_int, c_size_t, c_uint, c_uint32,
+from ctypes import (POINTER, c_char_p, c_double, c_float, c_int, c_longlong, c_size_t, c_uint, c_uint32,
                     c_void_p)
 
 import numpy as np
@@ -22,10 +22,14 @@ __all__ = [
     "sgprs_unpack_conv_weights", "sgprs_conv2d_workspace", "sgprs_conv2d", "sgprs_maxpool2d",
     "sgprs_conv_tuning_override", "sgprs_conv2d_plan", "sgprs_bn_relu", "sgprs_add_relu", "sgprs_avgpool_fc", "sgprs_global_avgpool", "sgprs_avgpool_fc_static",
     "sgprs_kernel_name",
+    "SGPRS_ACT_NONE", "SGPRS_ACT_RELU", "SGPRS_ACT_GELU", "SGPRS_ACT_SILU", "LinearDesc", "GroupNormDesc", "AttentionDesc",
+    "sgprs_linear_workspace", "sgprs_linear", "sgprs_group_norm_workspace", "sgprs_group_norm", "sgprs_attention_workspace",
+    "sgprs_attention",
 ]
 
 SGPRS_F32, SGPRS_BF16 = 0, 1
 SGPRS_POOL_OVERSUBSCRIBE, SGPRS_POOL_BLOCKED_LAYOUT = 1, 2
+SGPRS_ACT_NONE, SGPRS_ACT_RELU, SGPRS_ACT_GELU, SGPRS_ACT_SILU = 0, 1, 2, 3
 ERR_NAMES = {-1: "INVALID_ARG", -2: "NO_DEVICE", -3: "HIP", -4: "OOM", -5: "UNSUPPORTED", -6: "OVERSUBSCRIBED"}
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -39,6 +43,22 @@ class SgprsError(RuntimeError):
 
 class ConvDesc(ctypes.Structure):
     _fields_ = [(n, c_int) for n in ("n", "h", "w", "cin", "cout", "r", "s", "stride", "pad", "dtype", "relu")]
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("m", "n", "k", "dtype", "act", "residual_first")] + \
+               [(n, c_longlong) for n in ("ldx", "ldw", "ldr", "ldy")]
+
+
+class GroupNormDesc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("n", "hw", "c", "groups", "dtype", "act")] + [("eps", c_float)] + \
+               [(n, c_longlong) for n in ("ldx", "ldr", "ldy")]
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("n_seqs", "total_q", "total_kv", "max_q", "max_kv", "heads", "kv_heads", "head_dim", "dtype",
+                                     "causal")] + [("scale", c_float)] + \
+               [(n, c_longlong) for n in ("ldq", "ldk", "ldv", "ldo", "hq", "hk", "hv", "ho")]
 
 
 class _Params(ctypes.Structure):
@@ -115,6 +135,12 @@ def lib():
         "sgprs_avgpool_fc": (c_int, [c_int, c_int, c_int, c_int, c_int, vp, vp, vp, vp, vp, vp, c_int]),
         "sgprs_avgpool_fc_static": (c_int, [c_int, c_int, c_int, c_int, c_int, vp, vp, vp, vp, vp, c_int]),
         "sgprs_global_avgpool": (c_int, [c_int, c_int, c_int, c_int, vp, vp, vp, c_int]),
+        "sgprs_linear_workspace": (c_int, [POINTER(LinearDesc), c_int, POINTER(c_size_t)]),
+        "sgprs_linear": (c_int, [POINTER(LinearDesc), vp, vp, vp, vp, vp, vp, c_size_t, vp, c_int]),
+        "sgprs_group_norm_workspace": (c_int, [POINTER(GroupNormDesc), c_int, POINTER(c_size_t)]),
+        "sgprs_group_norm": (c_int, [POINTER(GroupNormDesc), vp, vp, vp, vp, vp, vp, c_size_t, vp, c_int]),
+        "sgprs_attention_workspace": (c_int, [POINTER(AttentionDesc), c_int, POINTER(c_size_t)]),
+        "sgprs_attention": (c_int, [POINTER(AttentionDesc), vp, vp, vp, vp, vp, vp, vp, c_size_t, vp, c_int]),
         "sgprs_task_create_resnet18": (c_int, [c_int, c_int, c_int, POINTER(_Params), POINTER(vp)]),
         "sgprs_task_destroy": (c_int, [vp]),
         "sgprs_task_num_stages": (c_int, [vp]),
@@ -389,6 +415,60 @@ def sgprs_avgpool_fc_static(dtype: int, n: int, hw: int, cin: int, cout: int, x:
     rc = (_native or _calls()).avgpool_fc_static(dtype, n, hw, cin, cout, x, w, bias, logits, pool.address if pool.__class__ is Pool else _address(_h(pool)), partition)
     if rc is None:
         rc = lib().sgprs_avgpool_fc_static(dtype, n, hw, cin, cout, x, w, bias, logits, _h(pool), partition)
+    if rc:
+        _check(rc)
+
+
+def _workspace(fn, desc, partition_cus: int) -> int:
+    n = c_size_t(0)
+    _check(fn(ctypes.byref(desc), partition_cus, ctypes.byref(n)))
+    return n.value
+
+
+def sgprs_linear_workspace(desc: LinearDesc, partition_cus: int) -> int:
+    return _workspace(lib().sgprs_linear_workspace, desc, partition_cus)
+
+
+def sgprs_linear(desc: LinearDesc, x: int, w: int, bias: int | None, residual: int | None, y: int, workspace: int | None,
+                 workspace_bytes: int, pool, partition: int) -> None:
+    rc = None
+    if desc.__class__ is LinearDesc:
+        rc = (_native or _calls()).linear(ctypes.addressof(desc), x, w, bias, residual, y, workspace, workspace_bytes,
+                                          pool.address if pool.__class__ is Pool else _address(_h(pool)), partition)
+    if rc is None:
+        rc = lib().sgprs_linear(ctypes.byref(desc), x, w, bias, residual, y, workspace, workspace_bytes, _h(pool), partition)
+    if rc:
+        _check(rc)
+
+
+def sgprs_group_norm_workspace(desc: GroupNormDesc, partition_cus: int) -> int:
+    return _workspace(lib().sgprs_group_norm_workspace, desc, partition_cus)
+
+
+def sgprs_group_norm(desc: GroupNormDesc, x: int, gamma: int | None, beta: int | None, residual: int | None, y: int,
+                     workspace: int | None, workspace_bytes: int, pool, partition: int) -> None:
+    rc = None
+    if desc.__class__ is GroupNormDesc:
+        rc = (_native or _calls()).group_norm(ctypes.addressof(desc), x, gamma, beta, residual, y, workspace, workspace_bytes,
+                                              pool.address if pool.__class__ is Pool else _address(_h(pool)), partition)
+    if rc is None:
+        rc = lib().sgprs_group_norm(ctypes.byref(desc), x, gamma, beta, residual, y, workspace, workspace_bytes, _h(pool), partition)
+    if rc:
+        _check(rc)
+
+
+def sgprs_attention_workspace(desc: AttentionDesc, partition_cus: int) -> int:
+    return _workspace(lib().sgprs_attention_workspace, desc, partition_cus)
+
+
+def sgprs_attention(desc: AttentionDesc, q: int, k: int, v: int, q_offsets: int, kv_offsets: int, o: int, workspace: int | None,
+                    workspace_bytes: int, pool, partition: int) -> None:
+    rc = None
+    if desc.__class__ is AttentionDesc:
+        rc = (_native or _calls()).attention(ctypes.addressof(desc), q, k, v, q_offsets, kv_offsets, o, workspace, workspace_bytes,
+                                             pool.address if pool.__class__ is Pool else _address(_h(pool)), partition)
+    if rc is None:
+        rc = lib().sgprs_attention(ctypes.byref(desc), q, k, v, q_offsets, kv_offsets, o, workspace, workspace_bytes, _h(pool), partition)
     if rc:
         _check(rc)
 

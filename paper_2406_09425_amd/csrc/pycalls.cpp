@@ -64,6 +64,15 @@ METHOD(avgpool_fc_static, 11, int dt = a.i(); int nn = a.i(); int hw = a.i(); in
        sgprs_avgpool_fc_static(dt, nn, hw, cin, cout, x, w, bias, lg, pool, part))
 METHOD(global_avgpool, 8, int dt = a.i(); int nn = a.i(); int hw = a.i(); int c = a.i(); auto* x = a.p(); auto* y = a.p<float>();
        auto* pool = a.p<sgprs_pool_t>(); int part = a.i(), sgprs_global_avgpool(dt, nn, hw, c, x, y, pool, part))
+METHOD(linear, 10, auto* d = a.p<sgprs_linear_desc_t>(); auto* x = a.p(); auto* w = a.p(); auto* bias = a.p<float>(); auto* res = a.p();
+       auto* y = a.p(); auto* ws = a.p(); size_t wb = a.z(); auto* pool = a.p<sgprs_pool_t>(); int part = a.i(),
+       sgprs_linear(d, x, w, bias, res, y, ws, wb, pool, part))
+METHOD(group_norm, 10, auto* d = a.p<sgprs_group_norm_desc_t>(); auto* x = a.p(); auto* ga = a.p<float>(); auto* be = a.p<float>();
+       auto* res = a.p(); auto* y = a.p(); auto* ws = a.p(); size_t wb = a.z(); auto* pool = a.p<sgprs_pool_t>(); int part = a.i(),
+       sgprs_group_norm(d, x, ga, be, res, y, ws, wb, pool, part))
+METHOD(attention, 11, auto* d = a.p<sgprs_attention_desc_t>(); auto* q = a.p(); auto* k = a.p(); auto* v = a.p(); auto* qo = a.p<int>();
+       auto* ko = a.p<int>(); auto* o = a.p(); auto* ws = a.p(); size_t wb = a.z(); auto* pool = a.p<sgprs_pool_t>(); int part = a.i(),
+       sgprs_attention(d, q, k, v, qo, ko, o, ws, wb, pool, part))
 METHOD(stage_run, 7, auto* t = a.p<sgprs_task_t>(); int st = a.i(); int b = a.i(); auto* in = a.p(); auto* out = a.p();
        auto* pool = a.p<sgprs_pool_t>(); int part = a.i(), sgprs_stage_run(t, st, b, in, out, pool, part))
 METHOD(task_run, 6, auto* t = a.p<sgprs_task_t>(); int b = a.i(); auto* in = a.p(); auto* lg = a.p<float>();
@@ -71,7 +80,7 @@ METHOD(task_run, 6, auto* t = a.p<sgprs_task_t>(); int b = a.i(); auto* in = a.p
 
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(conv2d), ENTRY(maxpool2d), ENTRY(bn_relu), ENTRY(add_relu), ENTRY(avgpool_fc), ENTRY(avgpool_fc_static),
-                         ENTRY(global_avgpool), ENTRY(stage_run), ENTRY(task_run), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(global_avgpool), ENTRY(linear), ENTRY(group_norm), ENTRY(attention), ENTRY(stage_run), ENTRY(task_run), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "Hot entry points of libsgprs.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
