@@ -47,6 +47,8 @@ int check_group_norm(const sgprs_group_norm_desc_t* d, sgprs_group_norm_desc_t* 
     if (d->n < 0 || d->hw <= 0 || d->c <= 0 || d->groups <= 0)
         return fail(SGPRS_ERR_INVALID_ARG, "n %d, hw %d, c %d, groups %d: need n >= 0 and the others > 0", d->n, d->hw, d->c, d->groups);
     if (d->c % d->groups) return fail(SGPRS_ERR_INVALID_ARG, "%d channels do not form %d equal groups", d->c, d->groups);
+    if ((long long)(d->c / d->groups) * (long long)dtype_size(d->dtype) > 16384)
+        return fail(SGPRS_ERR_UNSUPPORTED, "groups of %d channels: supported are up to 16 KiB of a position", d->c / d->groups);
     if (!(d->eps >= 0.f) || d->eps > 3e38f) return fail(SGPRS_ERR_INVALID_ARG, "eps %g is not a finite number >= 0", (double)d->eps);
     *full = *d;
     if ((rc = fill_stride("ldx", &full->ldx, d->c)) || (rc = fill_stride("ldr", &full->ldr, d->c)) || (rc = fill_stride("ldy", &full->ldy, d->c)))

@@ -1,78 +1,516 @@
-// Group norm with an activation, channels last.
+// Group norm with an activation (and residual), channels last.
 //
-// One workgroup per image and group: mean, then the squares of the deviations, then the results.
+// Bound by the memory: x in, y out.  A thread keeps to one vector of 16 bytes of channels and takes every
+// step-th position of it, so that whatever the groups' width, rows are read whole and what a thread knows of
+// its channels (mean, scale, shift) stays in registers.  Statistics are two passes over values in registers
+// (sum, then squares of the deviations from the mean), so nothing cancels, whatever the mean:
+//   * one launch where an image's positions of a slice of whole groups fit one workgroup's registers;
+//   * else one launch for the statistics of chunks of positions (mean and sum of squares of each group, in the
+//     workspace) and one that merges an image's chunks and writes the results;
+//   * a norm over all channels of single positions (layer norm) is a wavefront per row.
+#include <algorithm>
+
 #include "block_ops.h"
 
 namespace sgprs {
 
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+
 struct NormArgs {
-    const void* x;
+    const unsigned char* x;
     const float *gamma, *beta;
-    const void* residual;
-    void* y;
-    int hw, c, groups;
+    const unsigned char* residual;
+    unsigned char* y;
+    float2* partial;         // [image][chunk][group]: mean, sum of the squared deviations
+    int n, hw, c, groups, per;
+    unsigned per_mul;
+    int per_sh;              // channel / per
+    long long ldx, ldr, ldy; // bytes
     float eps;
-    long long ldx, ldr, ldy;
+    int slice, vectors, step;  // channels of a slice, vectors of 16 bytes in it, positions that a workgroup takes at once
+    unsigned vec_mul;
+    int vec_sh;              // thread / vectors
+    int slice_groups;
+    int chunks;              // of an image's positions
 };
 
-__device__ __forceinline__ float block_sum(float v, float* parts)
+__device__ __forceinline__ int div_magic(int m, unsigned mul, int sh) { return (int)(__umulhi(2u * (unsigned)m, mul) >> sh); }
+
+// WHOLE: the channels of every slice are whole vectors.  16-byte accesses need no alignment beyond the element's.
+template <int DT, bool WHOLE> struct NormVec {
+    static constexpr int ES = DT == SGPRS_BF16 ? 2 : 4, V = 16 / ES;
+    // the first `live` of V channels at p
+    static __device__ __forceinline__ u32x4_t load(const unsigned char* p, int live)
+    {
+        u32x4_t v = {0, 0, 0, 0};
+        if (WHOLE || live == V) {
+            __builtin_memcpy(&v, p, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if (e >= live) continue;
+                if constexpr (ES == 2) v[e / 2] |= (unsigned)((const unsigned short*)p)[e] << (e % 2 * 16);
+                else v[e] = ((const unsigned*)p)[e];
+            }
+        }
+        return v;
+    }
+    static __device__ __forceinline__ void store(unsigned char* p, u32x4_t v, int live)
+    {
+        if (WHOLE || live == V) {
+            __builtin_memcpy(p, &v, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if (e >= live) continue;
+                if constexpr (ES == 2) ((unsigned short*)p)[e] = (unsigned short)(v[e / 2] >> (e % 2 * 16));
+                else ((unsigned*)p)[e] = v[e];
+            }
+        }
+    }
+    // V floats of a per-channel array (NULL: `other`)
+    static __device__ __forceinline__ void per_channel(const float* p, int live, float other, float* out)
+    {
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[e] = other;
+        if (!p) return;
+        if (WHOLE || live == V) {
+            __builtin_memcpy(out, p, V * 4);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (e < live) out[e] = p[e];
+        }
+    }
+    static __device__ __forceinline__ float get(const u32x4_t& v, int e)
+    {
+        if constexpr (ES == 4) return __uint_as_float(v[e]);
+        else return __uint_as_float(e % 2 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
+    }
+    static __device__ __forceinline__ u32x4_t pack(const float* f)
+    {
+        u32x4_t v;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            if constexpr (ES == 4) v[p] = __float_as_uint(f[p]);
+            else v[p] = pack_bf16x2_relu(f[2 * p], f[2 * p + 1], kNoReluFloor);
+        }
+        return v;
+    }
+};
+
+// (x - mean) * scale + shift (+ residual), activated and stored, for one vector.
+template <int DT, int ACT, bool WHOLE>
+__device__ __forceinline__ void finish_vector(const NormArgs& a, const u32x4_t& x, const u32x4_t& r, const float* mean, const float* scale,
+                                              const float* shift, unsigned char* y, int live)
+{
+    typedef NormVec<DT, WHOLE> N;
+    float o[N::V];
+#pragma unroll
+    for (int e = 0; e < N::V; ++e) {
+        float z = (N::get(x, e) - mean[e]) * scale[e] + shift[e];
+        if (a.residual) z += N::get(r, e);
+        o[e] = activate<DT, ACT>(z);
+    }
+    N::store(y, N::pack(o), live);
+}
+
+// Sums over a workgroup, group by group: thread (s, v) brings V values of vector v (zeros for channels that do
+// not exist and threads that have none); total[g] gets the sum of group g of the slice.  scratch: a float for
+// every value, and one for every thread.  All threads call it; the order is fixed.
+template <int V>
+__device__ __forceinline__ void group_sums(const NormArgs& a, const float* value, int groups, float* scratch, float* total)
+{
+    const int tid = threadIdx.x, T = blockDim.x;
+    float* parts = scratch + T * V;
+    const bool whole = a.per % V == 0;  // a vector lies within one group
+    if (whole) {
+        float s = value[0];
+#pragma unroll
+        for (int e = 1; e < V; ++e) s += value[e];
+        scratch[tid] = s;
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) scratch[tid * V + e] = value[e];
+    }
+    __syncthreads();
+    const int row = whole ? a.vectors : a.vectors * V, width = whole ? a.per / V : a.per;  // of a position's values, of a group's
+    for (int g0 = 0; g0 < groups; g0 += T) {  // more groups than threads: in rounds
+        const int now = min(groups - g0, T), share = T / now;
+        const int g = tid % now, part = tid / now;
+        if (part < share) {
+            float s = 0.f;
+            const int at = (g0 + g) * width;
+            for (int p = part; p < a.step; p += share)
+                for (int i = 0; i < width; ++i) s += scratch[p * row + at + i];
+            parts[part * now + g] = s;
+        }
+        __syncthreads();
+        if (tid < now) {
+            float s = 0.f;
+            const int used = min(share, a.step);
+            for (int p = 0; p < used; ++p) s += parts[p * now + tid];
+            total[g0 + tid] = s;
+        }
+        __syncthreads();
+    }
+}
+
+// A workgroup's share: positions `first` and on of an image, channels c0 and on; a thread's vector and first position.
+// Loads of positions past the end repeat the last one, so that they need no branch; threads beyond the last whole
+// step repeat vector 0.
+template <int DT, bool WHOLE, int NV> struct NormShare {
+    typedef NormVec<DT, WHOLE> N;
+    int c0, channels, groups, image, first, rows, s, v, live;
+    long long row0;
+    __device__ __forceinline__ NormShare(const NormArgs& a)
+    {
+        const int tid = threadIdx.x;
+        c0 = blockIdx.x * a.slice;
+        channels = min(a.slice, a.c - c0);
+        groups = a.slice_groups;
+        if (channels < a.slice) groups = channels / a.per;
+        image = blockIdx.z;
+        first = blockIdx.y * a.step * NV;
+        rows = min(a.step * NV, a.hw - first);
+        s = div_magic(tid, a.vec_mul, a.vec_sh);
+        v = tid - s * a.vectors;
+        live = s < a.step ? min(N::V, channels - v * N::V) : 0;
+        if (WHOLE && channels < a.slice && v * N::V >= channels) live = 0;
+        row0 = (long long)image * a.hw + first;
+    }
+    __device__ __forceinline__ bool has(const NormArgs& a, int k) const { return live > 0 && s + k * a.step < rows; }
+    __device__ __forceinline__ void load(const NormArgs& a, const unsigned char* base, long long ld, u32x4_t* x) const
+    {
+        const unsigned char* p = base + row0 * ld + (long long)(c0 + (live > 0 ? v * N::V : 0)) * N::ES;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) x[k] = N::load(p + min(s + k * a.step, rows - 1) * ld, live);
+    }
+};
+
+// Statistics of a chunk of positions and a slice of channels, NV positions a thread; with FUSED the chunk is the
+// image and the results follow from the registers.
+template <int DT, int ACT, bool WHOLE, int NV, bool FUSED> __global__ __launch_bounds__(1024) void group_norm_chunk_kernel(const NormArgs a)
+{
+    typedef NormVec<DT, WHOLE> N;
+    constexpr int V = N::V;
+    extern __shared__ __align__(16) float lds[];
+    const int tid = threadIdx.x, T = blockDim.x;
+    const NormShare<DT, WHOLE, NV> m(a);
+    float* total = lds + T * (V + 1);  // per group of the slice
+    u32x4_t x[NV], r[FUSED ? NV : 1];
+    m.load(a, a.x, a.ldx, x);
+    if constexpr (FUSED) {
+        if (a.residual) m.load(a, a.residual, a.ldr, r);
+    }
+    float gamma[V], beta[V];
+    const int c = m.c0 + (m.live > 0 ? m.v * V : 0);
+    if constexpr (FUSED) {
+        N::per_channel(a.gamma ? a.gamma + c : nullptr, m.live, 1.f, gamma);
+        N::per_channel(a.beta ? a.beta + c : nullptr, m.live, 0.f, beta);
+    }
+    float sum[V], sq[V], mean[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[e] = sq[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[e] += m.has(a, k) ? N::get(x[k], e) : 0.f;
+    group_sums<V>(a, sum, m.groups, lds, total);
+    const float inv_count = 1.f / ((float)m.rows * (float)a.per);
+    int group[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        group[e] = div_magic(max(0, min(m.v * V + e, m.channels - 1)), a.per_mul, a.per_sh);
+        mean[e] = total[group[e]] * inv_count;
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float t = N::get(x[k], e) - mean[e];
+            sq[e] += (WHOLE || e < m.live) && m.has(a, k) ? t * t : 0.f;
+        }
+    float2* partial = a.partial + ((long long)m.image * a.chunks + blockIdx.y) * a.groups + blockIdx.x * a.slice_groups;
+    if constexpr (!FUSED) {
+        for (int g = tid; g < m.groups; g += T) partial[g].x = total[g] * inv_count;
+    }
+    __syncthreads();  // total has been read and is written again
+    group_sums<V>(a, sq, m.groups, lds, total);
+    if constexpr (!FUSED) {
+        for (int g = tid; g < m.groups; g += T) partial[g].y = total[g];
+    } else if (m.live > 0) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) gamma[e] *= 1.f / sqrtf(total[group[e]] * inv_count + a.eps);
+        unsigned char* yp = a.y + m.row0 * a.ldy + (long long)c * N::ES;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (m.has(a, k)) finish_vector<DT, ACT, WHOLE>(a, x[k], r[k], mean, gamma, beta, yp + (m.s + k * a.step) * a.ldy, m.live);
+    }
+}
+
+// Merges an image's chunks and writes the results of one of them.
+template <int DT, int ACT, bool WHOLE, int NV> __global__ __launch_bounds__(1024) void group_norm_apply_kernel(const NormArgs a)
+{
+    typedef NormVec<DT, WHOLE> N;
+    constexpr int V = N::V;
+    extern __shared__ __align__(16) float lds[];
+    const int tid = threadIdx.x, T = blockDim.x;
+    const NormShare<DT, WHOLE, NV> m(a);
+    const int groups = m.groups, full = a.step * NV;
+    u32x4_t x[NV], r[NV];
+    m.load(a, a.x, a.ldx, x);
+    if (a.residual) m.load(a, a.residual, a.ldr, r);
+    float gamma[V], beta[V], mean[V];
+    const int c = m.c0 + (m.live > 0 ? m.v * V : 0);
+    N::per_channel(a.gamma ? a.gamma + c : nullptr, m.live, 1.f, gamma);
+    N::per_channel(a.beta ? a.beta + c : nullptr, m.live, 0.f, beta);
+    // Chunks of a group: `share` threads, then their results in order.  All chunks but the last count `full` positions.
+    const float2* partial = a.partial + (long long)m.image * a.chunks * a.groups + blockIdx.x * a.slice_groups;
+    float *parts = lds, *means = lds + T, *scales = means + groups;
+    const float inv_hw = 1.f / (float)a.hw;
+    const int last = a.hw - (a.chunks - 1) * full;
+    for (int g0 = 0; g0 < groups; g0 += T) {
+        const int now = min(groups - g0, T), share = T / now, g = tid % now, part = tid / now;
+        const bool in = part < share;
+        const int used = min(share, a.chunks);
+        float t = 0.f;
+        if (in)
+            for (int k = part; k < a.chunks; k += share) t += partial[(long long)k * a.groups + g0 + g].x * (float)(k == a.chunks - 1 ? last : full);
+        __syncthreads();
+        if (in) parts[part * now + g] = t;
+        __syncthreads();
+        float mean = 0.f;
+        if (in) {
+            for (int p = 0; p < used; ++p) mean += parts[p * now + g];
+            mean *= inv_hw;
+        }
+        t = 0.f;
+        if (in)
+            for (int k = part; k < a.chunks; k += share) {
+                const float2 one = partial[(long long)k * a.groups + g0 + g];
+                t += one.y + (one.x - mean) * (one.x - mean) * ((float)(k == a.chunks - 1 ? last : full) * (float)a.per);
+            }
+        __syncthreads();
+        if (in) parts[part * now + g] = t;
+        __syncthreads();
+        if (tid < now) {
+            float m2 = 0.f;
+            for (int p = 0; p < used; ++p) m2 += parts[p * now + g];
+            means[g0 + tid] = mean;
+            scales[g0 + tid] = 1.f / sqrtf(m2 * inv_hw / (float)a.per + a.eps);
+        }
+    }
+    __syncthreads();
+    if (m.live <= 0) return;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        const int g = div_magic(min(m.v * V + e, m.channels - 1), a.per_mul, a.per_sh);
+        mean[e] = means[g];
+        gamma[e] *= scales[g];
+    }
+    unsigned char* yp = a.y + m.row0 * a.ldy + (long long)c * N::ES;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+        if (m.has(a, k)) finish_vector<DT, ACT, WHOLE>(a, x[k], r[k], mean, gamma, beta, yp + (m.s + k * a.step) * a.ldy, m.live);
+}
+
+__device__ __forceinline__ float wave_sum(float v)
 {
 #pragma unroll
     for (int s = 32; s; s >>= 1) v += __shfl_xor(v, s);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return (parts[0] + parts[1]) + (parts[2] + parts[3]);
+    return v;
 }
 
-template <int DT, int ACT> __global__ __launch_bounds__(256) void group_norm_kernel(const NormArgs a)
+// One group over single positions: a wavefront per row, NV vectors a lane, the next row requested before this one's sums.
+template <int DT, int ACT, bool WHOLE, int NV> __global__ __launch_bounds__(256) void row_norm_kernel(const NormArgs a)
 {
-    typedef typename ElemOf<DT>::type T;
-    __shared__ float parts[4];
-    const int per = a.c / a.groups;
-    const long long first = (long long)blockIdx.y * a.hw, total = (long long)a.hw * per;
-    const int c0 = blockIdx.x * per;
-    auto x = [&](long long i) { return (float)((const T*)a.x)[(first + i / per) * a.ldx + c0 + i % per]; };
-    float sum = 0.f;
-    for (long long i = threadIdx.x; i < total; i += 256) sum += x(i);
-    const float mean = block_sum(sum, parts) / (float)total;
-    float sq = 0.f;
-    for (long long i = threadIdx.x; i < total; i += 256) {
-        const float t = x(i) - mean;
-        sq += t * t;
+    typedef NormVec<DT, WHOLE> N;
+    constexpr int V = N::V;
+    const int lane = threadIdx.x & 63;
+    int c[NV], live[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        live[k] = max(0, min(V, a.c - (lane + 64 * k) * V));
+        c[k] = live[k] ? (lane + 64 * k) * V : 0;
     }
-    const float inv = 1.f / sqrtf(block_sum(sq, parts) / (float)total + a.eps);
-    for (long long i = threadIdx.x; i < total; i += 256) {
-        const int c = c0 + (int)(i % per);
-        const long long px = first + i / per;
-        float z = (x(i) - mean) * inv;
-        z = z * (a.gamma ? a.gamma[c] : 1.f) + (a.beta ? a.beta[c] : 0.f);
-        if (a.residual) z += (float)((const T*)a.residual)[px * a.ldr + c];
-        ((T*)a.y)[px * a.ldy + c] = (T)activate<ACT>(z);
+    auto load = [&](const unsigned char* base, long long ld, long long row, u32x4_t* x) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) x[k] = N::load(base + row * ld + c[k] * N::ES, live[k]);
+    };
+    const long long step = (long long)gridDim.x * 4;
+    long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= a.n) return;
+    u32x4_t x[NV], r[NV];
+    load(a.x, a.ldx, row, x);
+    if (a.residual) load(a.residual, a.ldr, row, r);
+    float gamma[NV][V], beta[NV][V];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        N::per_channel(a.gamma ? a.gamma + c[k] : nullptr, live[k], 1.f, gamma[k]);
+        N::per_channel(a.beta ? a.beta + c[k] : nullptr, live[k], 0.f, beta[k]);
+    }
+    const float inv_c = 1.f / (float)a.c;
+    for (;;) {
+        const long long next = row + step;
+        u32x4_t x1[NV], r1[NV];
+        if (next < a.n) {
+            load(a.x, a.ldx, next, x1);
+            if (a.residual) load(a.residual, a.ldr, next, r1);
+        }
+        float sum = 0.f, sq = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum += live[k] ? N::get(x[k], e) : 0.f;
+        const float mean1 = wave_sum(sum) * inv_c;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float t = N::get(x[k], e) - mean1;
+                sq += (WHOLE ? live[k] > 0 : e < live[k]) ? t * t : 0.f;
+            }
+        const float inv = 1.f / sqrtf(wave_sum(sq) * inv_c + a.eps);
+        float mean[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) mean[e] = mean1;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float scale[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) scale[e] = inv * gamma[k][e];
+            if (live[k]) finish_vector<DT, ACT, WHOLE>(a, x[k], r[k], mean, scale, beta[k], a.y + row * a.ldy + c[k] * N::ES, live[k]);
+        }
+        if (next >= a.n) return;
+        row = next;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            x[k] = x1[k];
+            r[k] = r1[k];
+        }
     }
 }
 
-size_t group_norm_workspace_bytes(const sgprs_group_norm_desc_t&, int) { return 0; }
+// ---- plans -------------------------------------------------------------------------------------
+struct NormPlan {
+    int rows;      // vectors a lane of the row kernel, 0: another kernel
+    bool fused;
+    int threads, nv, slice, vectors, step, chunks, slices;
+};
 
-template <int DT> static int launch_norm_typed(const NormArgs& a, int n, int act, hipStream_t stream)
+static NormPlan plan_norm(const sgprs_group_norm_desc_t& d, int cus)
 {
-    const dim3 grid(a.groups, n);
-    switch (act) {
-    case SGPRS_ACT_RELU: SGPRS_LAUNCH((group_norm_kernel<DT, SGPRS_ACT_RELU>), grid, 256, 0, stream, a); break;
-    case SGPRS_ACT_GELU: SGPRS_LAUNCH((group_norm_kernel<DT, SGPRS_ACT_GELU>), grid, 256, 0, stream, a); break;
-    case SGPRS_ACT_SILU: SGPRS_LAUNCH((group_norm_kernel<DT, SGPRS_ACT_SILU>), grid, 256, 0, stream, a); break;
-    default: SGPRS_LAUNCH((group_norm_kernel<DT, SGPRS_ACT_NONE>), grid, 256, 0, stream, a);
+    NormPlan p = {};
+    const int V = 16 / (int)dtype_size(d.dtype), per = d.c / d.groups;
+    if (d.hw == 1 && d.groups == 1 && d.c <= 64 * V * 8) {
+        const int need = (d.c + 64 * V - 1) / (64 * V);
+        p.rows = need <= 1 ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : 8;
+        return p;
+    }
+    auto vectors = [&](int slice) { return (slice + V - 1) / V; };
+    auto slice_of = [&](int bytes) {  // whole groups, at least so many bytes, whole vectors where that is possible
+        int s = (bytes / (int)dtype_size(d.dtype) + per - 1) / per * per;
+        for (int i = 0; i < V && s % V && s < d.c; ++i) s += per;
+        return std::min(s, d.c);
+    };
+    // one launch: the narrowest slices that keep rows of 64 bytes; wider ones where there are workgroups enough
+    constexpr int kMost = 1024 * 8;  // vectors in one workgroup's registers
+    for (int bytes : {512, 256, 128, 64}) {
+        const int s = slice_of(bytes), v = vectors(s), count = (d.c + s - 1) / s;
+        if (v > 1024) continue;
+        const long long need = (long long)(1024 / v) * 8;
+        if (d.hw > need) continue;
+        if (bytes > 64 && (long long)count * d.n < cus) continue;
+        p.fused = true;
+        p.slice = s;
+        break;
+    }
+    if (!p.fused) {
+        p.slice = d.c;
+        if (vectors(d.c) > 512) p.slice = std::max(per, 512 * V / per * per);
+    }
+    p.vectors = vectors(p.slice);
+    p.slices = (d.c + p.slice - 1) / p.slice;
+    if (p.fused) {
+        p.threads = 64;
+        auto holds = [&](int threads, int nv) { return threads >= p.vectors && (long long)(threads / p.vectors) * nv >= d.hw; };
+        while (p.threads < 1024 && !holds(p.threads, p.threads < 256 ? 1 : p.threads < 512 ? 2 : 4)) p.threads *= 2;
+        p.nv = 1;
+        while (p.nv < 8 && !holds(p.threads, p.nv)) p.nv *= 2;
+    } else {
+        p.threads = p.vectors > 512 ? 1024 : 512;
+        p.nv = 8;
+    }
+    p.step = std::max(1, p.threads / p.vectors);
+    p.chunks = (d.hw + p.step * p.nv - 1) / (p.step * p.nv);
+    return p;
+}
+
+size_t group_norm_workspace_bytes(const sgprs_group_norm_desc_t& d, int cus)
+{
+    const NormPlan p = plan_norm(d, cus);
+    return p.rows || p.fused ? 0 : (size_t)d.n * p.chunks * d.groups * sizeof(float2);
+}
+
+template <int DT, int ACT, bool WHOLE> static int launch_norm(const NormArgs& a, const NormPlan& p, int cus, hipStream_t stream)
+{
+    constexpr int V = NormVec<DT, WHOLE>::V;
+    if (p.rows) {
+        const dim3 grid(std::min((a.n + 3) / 4, 8 * cus));
+        switch (p.rows) {
+        case 1: SGPRS_LAUNCH((row_norm_kernel<DT, ACT, WHOLE, 1>), grid, 256, 0, stream, a); break;
+        case 2: SGPRS_LAUNCH((row_norm_kernel<DT, ACT, WHOLE, 2>), grid, 256, 0, stream, a); break;
+        case 4: SGPRS_LAUNCH((row_norm_kernel<DT, ACT, WHOLE, 4>), grid, 256, 0, stream, a); break;
+        default: SGPRS_LAUNCH((row_norm_kernel<DT, ACT, WHOLE, 8>), grid, 256, 0, stream, a);
+        }
+    } else {
+        const dim3 grid(p.slices, p.chunks, a.n);
+        const size_t lds = sizeof(float) * ((size_t)p.threads * (V + 1) + 2 * a.slice_groups);
+        if (p.fused) {
+            switch (p.nv) {
+            case 1: SGPRS_LAUNCH((group_norm_chunk_kernel<DT, ACT, WHOLE, 1, true>), grid, p.threads, lds, stream, a); break;
+            case 2: SGPRS_LAUNCH((group_norm_chunk_kernel<DT, ACT, WHOLE, 2, true>), grid, p.threads, lds, stream, a); break;
+            case 4: SGPRS_LAUNCH((group_norm_chunk_kernel<DT, ACT, WHOLE, 4, true>), grid, p.threads, lds, stream, a); break;
+            default: SGPRS_LAUNCH((group_norm_chunk_kernel<DT, ACT, WHOLE, 8, true>), grid, p.threads, lds, stream, a);
+            }
+        } else {
+            SGPRS_LAUNCH((group_norm_chunk_kernel<DT, SGPRS_ACT_NONE, WHOLE, 8, false>), grid, p.threads, lds, stream, a);
+            SGPRS_LAUNCH((group_norm_apply_kernel<DT, ACT, WHOLE, 8>), grid, p.threads, lds, stream, a);
+        }
     }
     SGPRS_HIP(hipGetLastError());
     return SGPRS_OK;
 }
 
+template <int DT, bool WHOLE> static int launch_norm_act(const NormArgs& a, const NormPlan& p, int act, int cus, hipStream_t stream)
+{
+    switch (act) {
+    case SGPRS_ACT_RELU: return launch_norm<DT, SGPRS_ACT_RELU, WHOLE>(a, p, cus, stream);
+    case SGPRS_ACT_GELU: return launch_norm<DT, SGPRS_ACT_GELU, WHOLE>(a, p, cus, stream);
+    case SGPRS_ACT_SILU: return launch_norm<DT, SGPRS_ACT_SILU, WHOLE>(a, p, cus, stream);
+    default: return launch_norm<DT, SGPRS_ACT_NONE, WHOLE>(a, p, cus, stream);
+    }
+}
+
 int launch_group_norm(const sgprs_group_norm_desc_t& d, const void* x, const float* gamma, const float* beta, const void* residual, void* y,
                       void* ws, hipStream_t stream, int cus)
 {
-    if (d.n > 65535) return fail(SGPRS_ERR_UNSUPPORTED, "%d images", d.n);
-    const NormArgs a = {x, gamma, beta, residual, y, d.hw, d.c, d.groups, d.eps, d.ldx, d.ldr, d.ldy};
-    return d.dtype == SGPRS_BF16 ? launch_norm_typed<SGPRS_BF16>(a, d.n, d.act, stream) : launch_norm_typed<SGPRS_F32>(a, d.n, d.act, stream);
+    const NormPlan p = plan_norm(d, cus);
+    if (!p.rows && (d.n > 65535 || p.chunks > 65535)) return fail(SGPRS_ERR_UNSUPPORTED, "%d images of %d positions", d.n, d.hw);
+    const long long es = (long long)dtype_size(d.dtype);
+    const int V = 16 / (int)es;
+    NormArgs a = {(const unsigned char*)x, gamma, beta, (const unsigned char*)residual, (unsigned char*)y, (float2*)ws, d.n, d.hw, d.c, d.groups,
+                  d.c / d.groups, 0, 0, d.ldx * es, d.ldr * es, d.ldy * es, d.eps, p.slice, p.vectors, p.step, 0, 0, 0, p.chunks};
+    div_constants(a.per, &a.per_mul, &a.per_sh);
+    if (!p.rows) {
+        div_constants(p.vectors, &a.vec_mul, &a.vec_sh);
+        a.slice_groups = p.slice / a.per;
+    }
+    const bool whole = d.c % V == 0 && (p.rows || p.slice % V == 0);
+    if (d.dtype == SGPRS_BF16)
+        return whole ? launch_norm_act<SGPRS_BF16, true>(a, p, d.act, cus, stream) : launch_norm_act<SGPRS_BF16, false>(a, p, d.act, cus, stream);
+    return whole ? launch_norm_act<SGPRS_F32, true>(a, p, d.act, cus, stream) : launch_norm_act<SGPRS_F32, false>(a, p, d.act, cus, stream);
 }
 
 }  // namespace sgprs

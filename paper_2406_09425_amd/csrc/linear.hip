@@ -103,7 +103,7 @@ template <int DT, int ACT> __device__ __forceinline__ void finish_row(const Line
     for (int e = 0; e < V; ++e) {
         const float re = ES == 4 ? __uint_as_float(r[e % 4]) : __uint_as_float(e % 2 ? r[e / 2] & 0xffff0000u : r[e / 2] << 16);
         const float t = z[e] + bias[e];
-        o[e] = a.residual_first ? activate<ACT>(t + re) : activate<ACT>(t) + re;
+        o[e] = a.residual_first ? activate<DT, ACT>(t + re) : activate<DT, ACT>(t) + re;
     }
     u32x4_t out;
 #pragma unroll
