@@ -30,6 +30,10 @@ struct AttentionArgs {
     int ldq, ldk, ldv, ldo;          // bytes
     long long hq, hk, hv, ho;        // bytes
     int slots;                       // query tiles, with room for each sequence's last one
+    int chunk, chunks;               // keys that a workgroup takes of a sequence; of the longest one
+    int row_blocks;                  // of 32 rows (queries x heads of a key head)
+    float* part_o;                   // [chunk][token][head][head_dim], weights relative to part_stat
+    float2* part_stat;               // [chunk][token][head]: maximum, sum
 };
 
 constexpr unsigned kOutside = 0x80000000u;  // beyond any descriptor's size: reads zeros
@@ -43,11 +47,12 @@ template <int DT, int HD> struct KvTile {
     static constexpr int CHUNKS = ROW / 16;
     static constexpr int KEYS = DT == SGPRS_BF16 ? 64 : 32;
     static constexpr int BYTES = KEYS * ROW;
-    static __device__ __forceinline__ int swizzle(int r)
+    // (linear in the bits of r: what is fixed of a read's row and chunk goes in as one exclusive or)
+    static __host__ __device__ constexpr int swizzle(int r)
     {
         if constexpr (ROW == 64) return (r >> 2) & 3;
         if constexpr (ROW == 128) return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
-        if constexpr (DT == SGPRS_BF16) return (r & 3) << 2 | ((r >> 2) & 3);
+        if constexpr (DT == SGPRS_BF16 && ROW == 256) return (r & 3) << 2 | ((r >> 2) & 3);
         return ((r >> 2) & 1) << 3 | ((r >> 3) & 1) << 2 | (r & 3);
     }
 };
@@ -59,32 +64,57 @@ typedef __attribute__((address_space(3))) unsigned lds_u32_t;
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 
 // One of the `parts` wavefronts' share of a tile: rows of a tensor that starts at p, `rows` of them, into LDS at `to`.
-template <int DT, int HD> __device__ __forceinline__ void request_tile(const unsigned char* p, int ld, int rows, int row_bytes, unsigned char* to, int part, int parts)
+template <int DT, int HD, int KEYS> __device__ __forceinline__ void request_tile(const unsigned char* p, int ld, int rows, int row_bytes, unsigned char* to, int part, int parts)
 {
     typedef KvTile<DT, HD> Tile;
-    constexpr int RPI = 1024 / Tile::ROW, LOADS = Tile::BYTES / 1024;  // rows of a load
-    const int lane = threadIdx.x & 63, lrow = lane / Tile::CHUNKS, slot = lane % Tile::CHUNKS;
-    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, rows > 0 ? (rows - 1) * ld + row_bytes : 0, 0x00020000);
+    constexpr int RPI = 1024 / Tile::ROW, LOADS = KEYS * Tile::ROW / 1024;  // rows of a load
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));  // the offsets are worked out in every tile rather than kept in registers
+    const int lrow = lane / Tile::CHUNKS, slot = (lane % Tile::CHUNKS) ^ Tile::swizzle(lrow);
+    const int size = __builtin_amdgcn_readfirstlane(rows > 0 ? (rows - 1) * ld + row_bytes : 0);  // (a clamp is vector arithmetic)
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, size, 0x00020000);
+    const unsigned first = (unsigned)(lrow * ld);
 #pragma unroll
     for (int i = 0; i < LOADS / parts; ++i) {
-        const int r = (i * parts + part) * RPI + lrow, chunk = slot ^ Tile::swizzle(r);
+        const int r = (i * parts + part) * RPI, chunk = (slot ^ Tile::swizzle(r)) << 4;  // r: of the load's first row
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr_t)(to + (i * parts + part) * 1024), 16,
-                                                 chunk * 16 < row_bytes ? (unsigned)(r * ld + chunk * 16) : kOutside, 0, 0, 0);
+                                                 chunk < row_bytes ? first + (unsigned)(r * ld) + (unsigned)chunk : kOutside, 0, 0, 0);
     }
 }
 
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
 
-// scores of 32 keys (rows `block` * 32 and on of the tile at `at`) with this lane's query
-template <int DT, int HD> __device__ __forceinline__ f32x16_t scores(unsigned at, int block, const u32x4_t* q)
+// Where a lane reads: its own row and chunk of a tile, to which a read adds fixed ones.  Hidden from the compiler in
+// every tile, or it would keep the sums for all reads in registers.
+template <int DT, int HD> struct LanePlaces {
+    typedef KvTile<DT, HD> Tile;
+    unsigned k, v;
+    __device__ __forceinline__ LanePlaces()
+    {
+        const int lane = threadIdx.x & 63, h = lane >> 5, s = lane & 15, g = (lane >> 4) & 1;
+        k = place(lane & 31, h);
+        if constexpr (DT == SGPRS_BF16) v = place(h * 4 + (s >> 2), g * 2 + ((s & 3) >> 1)) + (s & 1) * 8;
+        else v = place(h * 4, (lane & 31) >> 2) + (lane & 3) * 4;
+    }
+    static __device__ __forceinline__ unsigned place(int r, int chunk) { return (unsigned)(r * Tile::ROW + ((chunk ^ Tile::swizzle(r)) << 4)); }
+    static __device__ __forceinline__ unsigned hidden(unsigned base)
+    {
+        asm volatile("" : "+v"(base));
+        return base;
+    }
+    // row and chunk must not share bits with the lane's
+    static __device__ __forceinline__ unsigned plus(unsigned base, int r, int chunk) { return (base ^ (unsigned)((chunk ^ Tile::swizzle(r)) << 4)) + (unsigned)(r * Tile::ROW); }
+};
+
+// scores of 32 keys (rows `block` * 32 and on of a tile) with this lane's query
+template <int DT, int HD> __device__ __forceinline__ f32x16_t scores(unsigned k_base, int block, const u32x4_t* q)
 {
     typedef KvTile<DT, HD> Tile;
     constexpr int STEPS = HD * Tile::ES / 32;  // two chunks each
-    const int lane = threadIdx.x & 63, r = block * 32 + (lane & 31), h = lane >> 5;
     f32x16_t s = {};
 #pragma unroll
     for (int c = 0; c < STEPS; ++c) {
-        const u32x4_t k = *(const lds_u32x4_t*)(unsigned long)(at + r * Tile::ROW + (((2 * c + h) ^ Tile::swizzle(r)) << 4));
+        const u32x4_t k = *(const lds_u32x4_t*)(unsigned long)LanePlaces<DT, HD>::plus(k_base, block * 32, 2 * c);
         if constexpr (DT == SGPRS_BF16) {
             s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, q[c]), s, 0, 0, 0);
         } else {
@@ -96,15 +126,13 @@ template <int DT, int HD> __device__ __forceinline__ f32x16_t scores(unsigned at
 }
 
 // v of channels 32 d and on at keys 16 u of a block, as the row operand (bf16)
-template <int HD> __device__ __forceinline__ u32x4_t value_fragment(unsigned at, int block, int u, int d)
+template <int HD> __device__ __forceinline__ u32x4_t value_fragment(unsigned v_base, int block, int u, int d)
 {
-    typedef KvTile<SGPRS_BF16, HD> Tile;
-    const int lane = threadIdx.x & 63, s = lane & 15, h = lane >> 5, g = (lane >> 4) & 1;
     u32x4_t f;
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
-        const int r = block * 32 + u * 16 + a * 8 + h * 4 + (s >> 2), chunk = d * 4 + g * 2 + ((s & 3) >> 1);
-        const s16x4_t t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(unsigned long)(at + r * Tile::ROW + ((chunk ^ Tile::swizzle(r)) << 4) + (s & 1) * 8));
+        const s16x4_t t = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4_t*)(unsigned long)LanePlaces<SGPRS_BF16, HD>::plus(v_base, block * 32 + u * 16 + a * 8, d * 4));
         const u32x2_t w = __builtin_bit_cast(u32x2_t, t);
         f[2 * a] = w[0];
         f[2 * a + 1] = w[1];
@@ -112,13 +140,11 @@ template <int HD> __device__ __forceinline__ u32x4_t value_fragment(unsigned at,
     return f;
 }
 
-// o += V^T P^T for one block of 32 keys; p: this lane's 16 weights.  `masked`: some weights are zero because their
-// keys are not seen; should v hold infinities or NaNs there, 0 * v would be NaN, so such values are taken out of the
-// product and counted, in a second one, for the queries that see them.  seen: 1 or 0 for each weight.
-template <int DT, int HD>
-__device__ __forceinline__ void add_values(f32x16_t* o, const float* p, unsigned at, int block, bool masked, const float* seen)
+// o += V^T P^T for one block of 32 keys; p: this lane's 16 weights.  CLEAN: some keys are not seen, and where v holds
+// infinities or NaNs 0 * v would be NaN: such values are left out (*odd: there are some) for add_not_finite.
+template <int DT, int HD, bool CLEAN>
+__device__ __forceinline__ void add_values(f32x16_t* o, const float* p, unsigned v_base, int block, bool* odd)
 {
-    typedef KvTile<DT, HD> Tile;
     constexpr int DB = HD / 32;
     if constexpr (DT == SGPRS_BF16) {
         u32x4_t w[2];
@@ -130,60 +156,79 @@ __device__ __forceinline__ void add_values(f32x16_t* o, const float* p, unsigned
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                u32x4_t f = value_fragment<HD>(at, block, u, d);
-                if (masked) {
-                    bool odd = false;
+                u32x4_t f = value_fragment<HD>(v_base, block, u, d);
+                if constexpr (CLEAN) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) odd |= (f[e] & 0x7f80u) == 0x7f80u || (f[e] & 0x7f800000u) == 0x7f800000u;
-                    if (__any(odd)) {
-                        u32x4_t kind, sw;  // of each value that is not finite: 1 for inf, 2^8 for -inf, 2^16 for NaN
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            kind[e] = 0;
-#pragma unroll
-                            for (int half = 0; half < 2; ++half) {
-                                const unsigned v = f[e] >> (16 * half) & 0xffffu;
-                                if ((v & 0x7f80u) != 0x7f80u) continue;
-                                kind[e] |= (v & 0x7fu ? 0x4780u : v & 0x8000u ? 0x4380u : 0x3f80u) << (16 * half);
-                                f[e] &= ~(0xffffu << (16 * half));
-                            }
-                            sw[e] = pack_bf16x2_relu(seen[8 * u + 2 * e], seen[8 * u + 2 * e + 1], kNoReluFloor);
-                        }
-                        f32x16_t count = {};
-                        count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kind), __builtin_bit_cast(bf16x8_t, sw), count, 0, 0, 0);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const unsigned n = (unsigned)count[i];
-                            if (n) o[d][i] += n >> 16 || (n >> 8 && n & 0xffu) ? NAN : n >> 8 ? -INFINITY : INFINITY;
-                        }
+                    for (int e = 0; e < 4; ++e) {
+                        const bool lo = (f[e] & 0x7f80u) == 0x7f80u, hi = (f[e] & 0x7f800000u) == 0x7f800000u;
+                        f[e] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+                        *odd |= lo | hi;
                     }
                 }
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, f), __builtin_bit_cast(bf16x8_t, w[u]), o[d], 0, 0, 0);
             }
     } else {
-        const int lane = threadIdx.x & 63, h = lane >> 5;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const int r = block * 32 + (i >> 2) * 8 + h * 4 + (i & 3);
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
-                const int chunk = d * 8 + ((lane & 31) >> 2);
-                float f = __uint_as_float(*(const lds_u32_t*)(unsigned long)(at + r * Tile::ROW + ((chunk ^ Tile::swizzle(r)) << 4) + (lane & 3) * 4));
-                if (masked) {
-                    const bool odd = !(fabsf(f) < INFINITY);
-                    if (__any(odd)) {
-                        f32x16_t count = {};
-                        count = __builtin_amdgcn_mfma_f32_32x32x2f32(odd ? f != f ? 65536.f : f < 0.f ? 256.f : 1.f : 0.f, seen[i], count, 0, 0, 0);
-                        if (odd) f = 0.f;
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const unsigned n = (unsigned)count[j];
-                            if (n) o[d][j] += n >> 16 || (n >> 8 && n & 0xffu) ? NAN : n >> 8 ? -INFINITY : INFINITY;
-                        }
-                    }
+                float f = __uint_as_float(*(const lds_u32_t*)(unsigned long)LanePlaces<DT, HD>::plus(v_base, block * 32 + (i >> 2) * 8 + (i & 3), d * 8));
+                if constexpr (CLEAN) {
+                    const bool not_finite = !(fabsf(f) < INFINITY);
+                    f = not_finite ? 0.f : f;
+                    *odd |= not_finite;
                 }
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(f, p[i], o[d], 0, 0, 0);
             }
+        }
+    }
+}
+
+// Of a tile's keys, a lane sees those below this, counted from its half's first one.
+__device__ __forceinline__ int keys_left(int key0, int first_unseen)
+{
+    int left = first_unseen - key0 - (int)((threadIdx.x & 63) >> 5) * 4;
+    asm volatile("" : "+v"(left));  // compared with constants, not taken from 32 sums kept in registers
+    return left;
+}
+
+// What add_values left out of a block: infinities and NaNs reach the queries that see their key.  They are counted in
+// a product with 1 for a key that is seen and 0 for one that is not: infinities, + 2^8 for -infinities, + 2^16 for NaNs.
+template <int DT, int HD> __device__ __forceinline__ void add_not_finite(f32x16_t* o, unsigned v_base, int block, int key0, int first_unseen)
+{
+    const int mine = keys_left(key0, first_unseen);
+    auto seen = [&](int i) { return block * 32 + (i >> 2) * 8 + (i & 3) < mine ? 1.f : 0.f; };
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) {
+        f32x16_t count = {};
+        if constexpr (DT == SGPRS_BF16) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const u32x4_t f = value_fragment<HD>(v_base, block, u, d);
+                u32x4_t kind, w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    kind[e] = 0;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const unsigned v = f[e] >> (16 * half) & 0xffffu, k = v & 0x7fu ? 0x4780u : v & 0x8000u ? 0x4380u : 0x3f80u;
+                        kind[e] |= ((v & 0x7f80u) == 0x7f80u ? k : 0u) << (16 * half);
+                    }
+                    w[e] = pack_bf16x2_relu(seen(8 * u + 2 * e), seen(8 * u + 2 * e + 1), kNoReluFloor);
+                }
+                count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kind), __builtin_bit_cast(bf16x8_t, w), count, 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float f = __uint_as_float(*(const lds_u32_t*)(unsigned long)LanePlaces<DT, HD>::plus(v_base, block * 32 + (i >> 2) * 8 + (i & 3), d * 8));
+                count = __builtin_amdgcn_mfma_f32_32x32x2f32(fabsf(f) < INFINITY ? 0.f : f != f ? 65536.f : f < 0.f ? 256.f : 1.f, seen(i), count, 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const unsigned n = (unsigned)count[i];
+            o[d][i] += !n ? 0.f : n >> 16 || (n >> 8 && n & 0xffu) ? NAN : n >> 8 ? -INFINITY : INFINITY;
         }
     }
 }
@@ -193,6 +238,7 @@ template <int DT, int HD> struct Running {
     static constexpr int DB = HD / 32;
     f32x16_t o[DB];
     float top, sum;
+    LanePlaces<DT, HD> place;
     __device__ __forceinline__ void start()
     {
         top = -INFINITY;
@@ -200,19 +246,23 @@ template <int DT, int HD> struct Running {
 #pragma unroll
         for (int d = 0; d < DB; ++d) o[d] = f32x16_t{};
     }
-    // keys from `key` on are not seen; BLOCKS blocks of 32 from key0 on, at LDS address k_at and v_at
-    template <int BLOCKS> __device__ __forceinline__ void tile(const u32x4_t* q, float scale_log2, unsigned k_at, unsigned v_at, int key0, int first_unseen, bool masked)
+    // BLOCKS blocks of 32 keys from key0 on, in LDS at k_at and v_at; keys from first_unseen on are not seen.  k_done
+    // is called when k has been read, v_ready before v is.
+    template <int BLOCKS, bool MASKED, class KDone, class VReady>
+    __device__ __forceinline__ void tile(const u32x4_t* q, float scale_log2, unsigned k_at, unsigned v_at, int key0, int first_unseen, KDone k_done, VReady v_ready)
     {
-        const int h = (threadIdx.x & 63) >> 5;
+        const unsigned k_base = place.hidden(place.k + k_at), v_base = place.hidden(place.v + v_at);
         f32x16_t s[BLOCKS];
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) s[b] = scores<DT, HD>(k_base, b, q);
+        k_done();
+        const int mine = MASKED ? keys_left(key0, first_unseen) : 0;
         float most = -INFINITY;
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) {
-            s[b] = scores<DT, HD>(k_at, b, q);
-            if (masked) {
+            if constexpr (MASKED) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (key0 + b * 32 + (i >> 2) * 8 + h * 4 + (i & 3) >= first_unseen) s[b][i] = -INFINITY;
+                for (int i = 0; i < 16; ++i) s[b][i] = b * 32 + (i >> 2) * 8 + (i & 3) < mine ? s[b][i] : -INFINITY;
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) most = fmaxf(most, s[b][i]);
@@ -228,42 +278,72 @@ template <int DT, int HD> struct Running {
                 for (int i = 0; i < 16; ++i) o[d][i] *= keep;
         }
         const float base = top == -INFINITY ? 0.f : top + kKeepMax;  // weights stay below 1, so sums with large v keep their range
+        v_ready();
+        bool odd = false;
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) {
-            float p[16], seen[16];
+            float p[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale_log2, -base));
                 sum += p[i];
-                seen[i] = key0 + b * 32 + (i >> 2) * 8 + h * 4 + (i & 3) < first_unseen ? 1.f : 0.f;
             }
-            add_values<DT, HD>(o, p, v_at, b, masked, seen);
+            add_values<DT, HD, MASKED>(o, p, v_base, b, &odd);
+        }
+        if (MASKED && __any(odd)) {
+#pragma unroll 1
+            for (int b = 0; b < BLOCKS; ++b) add_not_finite<DT, HD>(o, v_base, b, key0, first_unseen);
         }
     }
 };
 #endif
 
+// 1 / the sum of the weights; without a key the result is zero, and where all scores are -inf there is none.
+__device__ __forceinline__ float normaliser(float sum, bool any_key) { return sum > 0.f ? 1.f / sum : any_key ? NAN : 0.f; }
+
+// four channels of a result, from channel c on
+template <int DT> __device__ __forceinline__ void store4(unsigned char* row, int c, const float* z)
+{
+    if constexpr (DT == SGPRS_BF16)
+        *(u32x2_t*)(row + c * 2) = u32x2_t{pack_bf16x2_relu(z[0], z[1], kNoReluFloor), pack_bf16x2_relu(z[2], z[3], kNoReluFloor)};
+    else
+        *(float4*)(row + c * 4) = make_float4(z[0], z[1], z[2], z[3]);
+}
+
+#if __HIP_DEVICE_COMPILE__
+// First token and length of a sequence, inside the tensor whatever the offsets say; in scalar registers, since buffer
+// descriptors are made of them.
+__device__ __forceinline__ void range_of(const int* offsets, int seq, int total, int* first, int* count)
+{
+    const int from = min(max(offsets[seq], 0), total), to = min(max(offsets[seq + 1], from), total);
+    *first = __builtin_amdgcn_readfirstlane(from);
+    *count = __builtin_amdgcn_readfirstlane(to - from);
+}
+#endif
+
 // Sequence and tile of a slot: a sequence's tiles start at slot q_offsets[s] / BM + s, which leaves each its own.
 __device__ __forceinline__ bool tile_of_slot(const AttentionArgs& a, int slot, int bm, int* seq, int* row, int* q0, int* nq)
 {
+#if __HIP_DEVICE_COMPILE__
     int lo = 0, hi = a.n_seqs;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (a.q_offsets[mid] / bm + mid <= slot) lo = mid;
         else hi = mid;
     }
-    const int first = min(max(a.q_offsets[lo], 0), a.total_q), end = min(max(a.q_offsets[lo + 1], first), a.total_q);
-    const int tile = slot - (a.q_offsets[lo] / bm + lo);
-    *seq = lo;
-    *q0 = first;
-    *nq = end - first;
+    *seq = __builtin_amdgcn_readfirstlane(lo);
+    range_of(a.q_offsets, *seq, a.total_q, q0, nq);
+    const int tile = __builtin_amdgcn_readfirstlane(slot - (a.q_offsets[*seq] / bm + *seq));
     *row = tile * bm;
     return tile >= 0 && tile < (1 << 24) && *row < *nq;
+#else
+    return false;
+#endif
 }
 
 // ---- prompts -----------------------------------------------------------------------------------
 // 128 queries of one head per workgroup, 32 per wavefront; tiles of keys double buffered in LDS.
-template <int DT, int HD> __global__ __launch_bounds__(256, 2) void attention_prompt_kernel(const AttentionArgs a)
+template <int DT, int HD> __global__ __launch_bounds__(256, (DT == SGPRS_F32 && HD > 64 ? 1 : 2)) void attention_prompt_kernel(const AttentionArgs a)
 {
 #if __HIP_DEVICE_COMPILE__
     typedef KvTile<DT, HD> Tile;
@@ -277,7 +357,8 @@ template <int DT, int HD> __global__ __launch_bounds__(256, 2) void attention_pr
     const int kv_head = j % a.kv_heads, head = kv_head * a.group + j / a.kv_heads;
     int seq, row0, q0, nq;
     if (!tile_of_slot(a, slot, BM, &seq, &row0, &q0, &nq)) return;
-    const int k0 = min(max(a.kv_offsets[seq], 0), a.total_kv), nk = min(max(a.kv_offsets[seq + 1], k0), a.total_kv) - k0;
+    int k0, nk;
+    range_of(a.kv_offsets, seq, a.total_kv, &k0, &nk);
     const int row = row0 + wave * 32 + (lane & 31);       // of the sequence
     const int last_row = min(row0 + BM, nq) - 1;
     const int keys = a.causal ? max(0, min(nk, last_row + nk - nq + 1)) : nk;  // that anyone here sees
@@ -300,8 +381,8 @@ template <int DT, int HD> __global__ __launch_bounds__(256, 2) void attention_pr
     auto request = [&](int t) {
         unsigned char* to = smem + (t & 1) * 2 * Tile::BYTES;
         const int rows = max(0, min(Tile::KEYS, nk - t * Tile::KEYS));
-        request_tile<DT, HD>(kp + (long long)t * Tile::KEYS * a.ldk, a.ldk, rows, row_bytes, to, wave, 4);
-        request_tile<DT, HD>(vp + (long long)t * Tile::KEYS * a.ldv, a.ldv, rows, row_bytes, to + Tile::BYTES, wave, 4);
+        request_tile<DT, HD, Tile::KEYS>(kp + (long long)t * Tile::KEYS * a.ldk, a.ldk, rows, row_bytes, to, wave, 4);
+        request_tile<DT, HD, Tile::KEYS>(vp + (long long)t * Tile::KEYS * a.ldv, a.ldv, rows, row_bytes, to + Tile::BYTES, wave, 4);
     };
     Running<DT, HD> run;
     run.start();
@@ -315,15 +396,16 @@ template <int DT, int HD> __global__ __launch_bounds__(256, 2) void attention_pr
         const unsigned at = (unsigned)((t & 1) * 2 * Tile::BYTES);
         const int key0 = t * Tile::KEYS;
         if (key0 < wave_any) {
-            if (key0 + Tile::KEYS <= wave_all) run.template tile<Tile::KEYS / 32>(q, a.scale_log2, at, at + Tile::BYTES, key0, first_unseen, false);
-            else run.template tile<Tile::KEYS / 32>(q, a.scale_log2, at, at + Tile::BYTES, key0, first_unseen, true);
+            auto nothing = [] {};
+            if (key0 + Tile::KEYS <= wave_all) run.template tile<Tile::KEYS / 32, false>(q, a.scale_log2, at, at + Tile::BYTES, key0, first_unseen, nothing, nothing);
+            else run.template tile<Tile::KEYS / 32, true>(q, a.scale_log2, at, at + Tile::BYTES, key0, first_unseen, nothing, nothing);
         }
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0xC07F);
     }
     if (row >= nq) return;
     const float sum = run.sum + other_half(run.sum);
-    const float inv = sum > 0.f ? 1.f / sum : first_unseen > 0 ? NAN : 0.f;
+    const float inv = normaliser(sum, first_unseen > 0);
     unsigned char* op = a.o + (long long)(q0 + row) * a.ldo + head * a.ho;
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d)
@@ -331,55 +413,291 @@ template <int DT, int HD> __global__ __launch_bounds__(256, 2) void attention_pr
         for (int i = 0; i < 16; i += 4) {
             const int c = d * 32 + (i >> 2) * 8 + h * 4;
             if (c >= a.head_dim) continue;
-            if constexpr (DT == SGPRS_BF16) {
-                *(u32x2_t*)(op + c * 2) = u32x2_t{pack_bf16x2_relu(run.o[d][i] * inv, run.o[d][i + 1] * inv, kNoReluFloor),
-                                                  pack_bf16x2_relu(run.o[d][i + 2] * inv, run.o[d][i + 3] * inv, kNoReluFloor)};
-            } else {
-                u32x4_t w;
+            float z[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(run.o[d][i + e] * inv);
-                *(u32x4_t*)(op + c * 4) = w;
-            }
+            for (int e = 0; e < 4; ++e) z[e] = run.o[d][i + e] * inv;
+            store4<DT>(op, c, z);
         }
 #endif
 }
 
-// ---- plans -------------------------------------------------------------------------------------
-size_t attention_workspace_bytes(const sgprs_attention_desc_t&, int) { return 0; }
+// ---- single tokens -----------------------------------------------------------------------------
+// Few queries against many keys: bound by reading k and v.  The queries of all heads that share a key head are one
+// block of 32 columns (or several), so k and v are read once for them; a workgroup takes a chunk of a sequence's
+// keys, its wavefronts every NW-th tile of 32 keys, each through LDS buffers of its own.  The wavefronts' sums meet
+// in LDS; those of several chunks in the workspace, joined by attention_join_kernel.
+template <int DT, int HD> struct DecodeShape {
+    static constexpr int HALF = 32 * KvTile<DT, HD>::ROW, STAGE = 2 * HALF;  // k, and v behind it
+    static constexpr int NW = 4;
+    static constexpr int SROW = HD + 4;                                       // floats of a row where the sums meet
+    static constexpr int JOIN = NW * (32 * SROW + 64) * 4, LDS = NW * STAGE > JOIN ? NW * STAGE : JOIN;
+};
 
-template <int DT, int HD> static int launch_prompt(AttentionArgs a, hipStream_t stream)
+template <int DT, int HD> __global__ __launch_bounds__((DecodeShape<DT, HD>::NW * 64), (DecodeShape<DT, HD>::LDS > 81920 ? 1 : 2)) void attention_decode_kernel(const AttentionArgs a)
 {
-    constexpr int lds = 4 * KvTile<DT, HD>::BYTES;
-    a.slots = a.total_q / 128 + a.n_seqs;
-    const long long grid = (long long)a.slots * a.heads;
+#if __HIP_DEVICE_COMPILE__
+    typedef KvTile<DT, HD> Tile;
+    typedef DecodeShape<DT, HD> Shape;
+    constexpr int ES = Tile::ES, STEPS = HD * ES / 32, NW = Shape::NW, LOADS = Shape::HALF / 1024;  // of k, of v
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int item = blockIdx.x;
+    const int kv_head = item % a.kv_heads;
+    item /= a.kv_heads;
+    const int block = item % a.row_blocks;
+    item /= a.row_blocks;
+    const int seq = item % a.n_seqs, chunk = item / a.n_seqs;
+    int q0, nq;
+    range_of(a.q_offsets, seq, a.total_q, &q0, &nq);
+    int k0, nk;
+    range_of(a.kv_offsets, seq, a.total_kv, &k0, &nk);
+    const int rows = nq * a.group - block * 32;  // (query, head of the group), heads fastest
+    if (rows <= 0 || (chunk > 0 && chunk * a.chunk >= nk)) return;
+    const int my = block * 32 + min(col, rows - 1), query = my / a.group, head = kv_head * a.group + my - query * a.group;
+    const int last_query = min(nq * a.group - 1, block * 32 + 31) / a.group;
+    const int first_unseen = a.causal ? min(nk, query + nk - nq + 1) : nk;
+    const int begin = chunk * a.chunk, end = max(begin, min(begin + a.chunk, a.causal ? min(nk, last_query + nk - nq + 1) : nk));
+    const int all = a.causal ? min(nk, block * 32 / a.group + nk - nq + 1) : nk;  // keys that every query of the block sees
+    const int row_bytes = a.head_dim * ES;
+
+    u32x4_t q[STEPS];
+    const unsigned char* qp = a.q + (long long)(q0 + query) * a.ldq + head * a.hq;
+#pragma unroll
+    for (int c = 0; c < STEPS; ++c) {
+        q[c] = (2 * c + h) * 16 < row_bytes ? *(const u32x4_t*)(qp + (2 * c + h) * 16) : u32x4_t{0, 0, 0, 0};
+        q[c] ^= a.q_flip;
+    }
+    const unsigned char* kp = a.k + (long long)(k0 + begin) * a.ldk + kv_head * a.hk;
+    const unsigned char* vp = a.v + (long long)(k0 + begin) * a.ldv + kv_head * a.hv;
+    const int tiles = (end - begin + 31) >> 5;
+    // One buffer for k and one for v: the next k is requested when the scores are there, the next v behind the products.
+    unsigned char* mine = smem + wave * Shape::STAGE;
+    const unsigned at = (unsigned)(wave * Shape::STAGE);
+    auto request_k = [&](int t) {
+        request_tile<DT, HD, 32>(kp + (long long)t * 32 * a.ldk, a.ldk, max(0, min(32, end - begin - t * 32)), row_bytes, mine, 0, 1);
+    };
+    auto request_v = [&](int t) {
+        request_tile<DT, HD, 32>(vp + (long long)t * 32 * a.ldv, a.ldv, max(0, min(32, end - begin - t * 32)), row_bytes, mine + Shape::HALF, 0, 1);
+    };
+    auto landed = [] {  // all but the last LOADS requests
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt((LOADS & 15) | ((LOADS >> 4) << 14) | 0x0F70);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto read = [] {  // what was read from LDS has arrived, the buffer may be written
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0xC07F);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    Running<DT, HD> run;
+    run.start();
+    request_k(wave);
+    request_v(wave);
+    for (int t = wave; t < tiles; t += NW) {
+        landed();
+        const int key0 = begin + t * 32;
+        auto k_done = [&] {
+            read();
+            request_k(t + NW);
+        };
+        if (key0 + 32 <= all) run.template tile<1, false>(q, a.scale_log2, at, at + Shape::HALF, key0, first_unseen, k_done, landed);
+        else run.template tile<1, true>(q, a.scale_log2, at, at + Shape::HALF, key0, first_unseen, k_done, landed);
+        read();
+        request_v(t + NW);
+    }
+    __builtin_amdgcn_s_waitcnt(0);  // requests past the end write zeros
+    __syncthreads();
+    float* sums = (float*)smem;  // [wavefront][column][channel], then [wavefront][column] maxima and sums
+    float* tops = sums + NW * 32 * Shape::SROW;
+    float* totals = tops + NW * 32;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            *(float4*)(sums + (wave * 32 + col) * Shape::SROW + d * 32 + (i >> 2) * 8 + h * 4) = make_float4(run.o[d][i], run.o[d][i + 1], run.o[d][i + 2], run.o[d][i + 3]);
+    const float sum = run.sum + other_half(run.sum);
+    if (h == 0) {
+        tops[wave * 32 + col] = run.top;
+        totals[wave * 32 + col] = sum;
+    }
+    __syncthreads();
+    const int live = min(rows, 32), vecs = a.head_dim >> 2;
+    const bool whole = nk <= a.chunk;
+    for (int e = threadIdx.x; e < live * vecs; e += NW * 64) {
+        const int r = e / vecs, c = (e - r * vecs) * 4;
+        float top = tops[r], total = 0.f, z[4] = {};
+#pragma unroll
+        for (int v = 1; v < NW; ++v) top = fmaxf(top, tops[v * 32 + r]);
+#pragma unroll
+        for (int v = 0; v < NW; ++v) {
+            const float t = tops[v * 32 + r], w = t == top ? 1.f : __builtin_amdgcn_exp2f(t - top);  // (both may be -inf: sums of 0)
+            total = __builtin_fmaf(totals[v * 32 + r], w, total);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) z[x] = __builtin_fmaf(sums[(v * 32 + r) * Shape::SROW + c + x], w, z[x]);
+        }
+        const int row = block * 32 + r, qi = row / a.group, hd = kv_head * a.group + row - qi * a.group;
+        if (whole) {
+            const float inv = normaliser(total, (a.causal ? min(nk, qi + nk - nq + 1) : nk) > 0);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) z[x] *= inv;
+            store4<DT>(a.o + (long long)(q0 + qi) * a.ldo + hd * a.ho, c, z);
+        } else {
+            const long long at = ((long long)chunk * a.total_q + q0 + qi) * a.heads + hd;
+            *(float4*)(a.part_o + at * a.head_dim + c) = make_float4(z[0], z[1], z[2], z[3]);
+            if (c == 0) a.part_stat[at] = make_float2(top, total);
+        }
+    }
+#endif
+}
+
+// Joins the chunks of sequences that have several: a workgroup per query and head, four channels a lane, eight
+// chunks at a time, added in a fixed order.
+constexpr int kMaxChunks = 512 + 2;  // of plan_attention, on the largest partition
+template <int DT> __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs a)
+{
+#if __HIP_DEVICE_COMPILE__
+    __shared__ float weight[kMaxChunks + 8];
+    __shared__ float stat[8];
+    __shared__ float4 part[8][32];
+    const int tid = threadIdx.x, lane = tid & 31, group = tid >> 5;
+    const int token = blockIdx.x / a.heads, head = blockIdx.x - token * a.heads;
+    int seq = 0, hi = a.n_seqs;  // the last sequence that does not begin behind the token
+    while (hi - seq > 1) {
+        const int mid = (seq + hi) >> 1;
+        if (a.q_offsets[mid] <= token) seq = mid;
+        else hi = mid;
+    }
+    int k0, nk;
+    range_of(a.kv_offsets, seq, a.total_kv, &k0, &nk);
+    if (nk <= a.chunk) return;
+    const int n = min(a.chunks, (nk + a.chunk - 1) / a.chunk);
+    const long long step = (long long)a.total_q * a.heads;
+    // maximum, weights and sum
+    float top = -INFINITY, total = 0.f;
+    for (int s = tid; s < n; s += 256) top = fmaxf(top, a.part_stat[s * step + blockIdx.x].x);
+#pragma unroll
+    for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    if ((tid & 63) == 0) stat[tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(stat[0], stat[1]), fmaxf(stat[2], stat[3]));
+    for (int s = tid; s < n; s += 256) {
+        const float2 st = a.part_stat[s * step + blockIdx.x];
+        const float w = st.x == top ? 1.f : __builtin_amdgcn_exp2f(st.x - top);
+        weight[s] = w;
+        total = __builtin_fmaf(st.y, w, total);
+    }
+#pragma unroll
+    for (int x = 32; x; x >>= 1) total += __shfl_xor(total, x);
+    if ((tid & 63) == 0) stat[4 + (tid >> 6)] = total;
+    __syncthreads();
+    total = (stat[4] + stat[5]) + (stat[6] + stat[7]);
+    float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int c = lane * 4;
+    if (c < a.head_dim) {
+        const float* p = a.part_o + (long long)blockIdx.x * a.head_dim + c;
+#pragma unroll 4
+        for (int s = group; s < n; s += 8) {
+            const float w = weight[s];
+            const float4 o = *(const float4*)(p + s * step * a.head_dim);
+            z = make_float4(__builtin_fmaf(o.x, w, z.x), __builtin_fmaf(o.y, w, z.y), __builtin_fmaf(o.z, w, z.z), __builtin_fmaf(o.w, w, z.w));
+        }
+    }
+    part[group][lane] = z;
+    __syncthreads();
+    if (group || c >= a.head_dim) return;
+    float out[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+    for (int g = 1; g < 8; ++g) {
+        const float4 t = part[g][lane];
+        out[0] += t.x;
+        out[1] += t.y;
+        out[2] += t.z;
+        out[3] += t.w;
+    }
+    const int query = token - a.q_offsets[seq], nq = a.q_offsets[seq + 1] - a.q_offsets[seq];
+    const float inv = normaliser(total, (a.causal ? min(nk, query + nk - nq + 1) : nk) > 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] *= inv;
+    store4<DT>(a.o + (long long)token * a.ldo + head * a.ho, c, out);
+#endif
+}
+
+// ---- plans -------------------------------------------------------------------------------------
+struct AttentionPlan {
+    bool decode;
+    int chunk, chunks, row_blocks;
+};
+
+static AttentionPlan plan_attention(const sgprs_attention_desc_t& d, int cus)
+{
+    AttentionPlan p = {};
+    p.decode = d.max_q <= 32;
+    p.chunk = std::max(1, d.max_kv);
+    p.chunks = 1;
+    if (p.decode) {
+        p.row_blocks = (d.max_q * (d.heads / d.kv_heads) + 31) / 32;
+        // Chunks of keys for a workgroup a CU, 128 keys (a tile for each wavefront) or more: 16 caches of 2048 tokens,
+        // 32/8 heads of 128, take 31.6 us so, 32.9 with two and 34.9 with three (more partial sums to join); one cache
+        // of 8192 12.7, 13.7 and 13.7.
+        const long long want = (long long)d.total_kv * d.kv_heads * p.row_blocks / cus;
+        p.chunk = (int)std::min<long long>(std::max<long long>(want + 127, 128) / 128 * 128, 1 << 30);
+        p.chunks = std::max(1, (d.max_kv + p.chunk - 1) / p.chunk);
+    }
+    return p;
+}
+
+size_t attention_workspace_bytes(const sgprs_attention_desc_t& d, int cus)
+{
+    const AttentionPlan p = plan_attention(d, cus);
+    return p.chunks > 1 ? (size_t)p.chunks * d.total_q * d.heads * (d.head_dim * sizeof(float) + sizeof(float2)) : 0;
+}
+
+template <auto kernel> static int launch_sized(long long grid, int threads, int lds, const AttentionArgs& a, hipStream_t stream)
+{
     if (grid >= (1ll << 31)) return fail(SGPRS_ERR_UNSUPPORTED, "%d sequences of %d tokens and %d heads", a.n_seqs, a.total_q, a.heads);
     static std::atomic<bool> raised{false};  // more than the default 64 KiB of dynamic LDS needs an opt-in per kernel
     if (lds > 65536 && !raised) {
-        SGPRS_HIP(hipFuncSetAttribute((const void*)attention_prompt_kernel<DT, HD>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+        SGPRS_HIP(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
         raised = true;
     }
-    SGPRS_LAUNCH((attention_prompt_kernel<DT, HD>), dim3((unsigned)grid), 256, lds, stream, a);
+    SGPRS_LAUNCH(kernel, dim3((unsigned)grid), threads, lds, stream, a);
     SGPRS_HIP(hipGetLastError());
     return SGPRS_OK;
 }
 
-template <int DT> static int launch_typed(const AttentionArgs& a, hipStream_t stream)
+template <int DT, int HD> static int launch_shape(AttentionArgs a, bool decode, hipStream_t stream)
 {
-    if (a.head_dim <= 32) return launch_prompt<DT, 32>(a, stream);
-    if (a.head_dim <= 64) return launch_prompt<DT, 64>(a, stream);
-    if (a.head_dim <= 96) return launch_prompt<DT, 96>(a, stream);
-    return launch_prompt<DT, 128>(a, stream);
+    if (!decode) {
+        a.slots = a.total_q / 128 + a.n_seqs;
+        return launch_sized<attention_prompt_kernel<DT, HD>>((long long)a.slots * a.heads, 256, 4 * KvTile<DT, HD>::BYTES, a, stream);
+    }
+    typedef DecodeShape<DT, HD> Shape;
+    const int rc = launch_sized<attention_decode_kernel<DT, HD>>((long long)a.chunks * a.n_seqs * a.row_blocks * a.kv_heads, Shape::NW * 64, Shape::LDS, a, stream);
+    if (rc || a.chunks == 1) return rc;
+    return launch_sized<attention_join_kernel<DT>>((long long)a.total_q * a.heads, 256, 0, a, stream);
+}
+
+template <int DT> static int launch_typed(const AttentionArgs& a, bool decode, hipStream_t stream)
+{
+    if (a.head_dim <= 32) return launch_shape<DT, 32>(a, decode, stream);
+    if (a.head_dim <= 64) return launch_shape<DT, 64>(a, decode, stream);
+    if (a.head_dim <= 96) return launch_shape<DT, 96>(a, decode, stream);
+    return launch_shape<DT, 128>(a, decode, stream);
 }
 
 int launch_attention(const sgprs_attention_desc_t& d, const void* q, const void* k, const void* v, const int* q_offsets, const int* kv_offsets,
                      void* o, void* ws, hipStream_t stream, int cus)
 {
     const long long es = (long long)dtype_size(d.dtype);
-    const AttentionArgs a = {(const unsigned char*)q, (const unsigned char*)k, (const unsigned char*)v, (unsigned char*)o, q_offsets, kv_offsets,
+    const AttentionPlan p = plan_attention(d, cus);
+    AttentionArgs a = {(const unsigned char*)q, (const unsigned char*)k, (const unsigned char*)v, (unsigned char*)o, q_offsets, kv_offsets,
                              d.n_seqs, d.total_q, d.total_kv, d.heads, d.kv_heads, d.heads / d.kv_heads, d.head_dim, d.causal,
                              std::fabs(d.scale) * 1.4426950408889634f, d.scale >= 0.f ? 0u : d.dtype == SGPRS_BF16 ? 0x80008000u : 0x80000000u,
-                             (int)(d.ldq * es), (int)(d.ldk * es), (int)(d.ldv * es), (int)(d.ldo * es), d.hq * es, d.hk * es, d.hv * es, d.ho * es, 0};
-    return d.dtype == SGPRS_BF16 ? launch_typed<SGPRS_BF16>(a, stream) : launch_typed<SGPRS_F32>(a, stream);
+                             (int)(d.ldq * es), (int)(d.ldk * es), (int)(d.ldv * es), (int)(d.ldo * es), d.hq * es, d.hk * es, d.hv * es, d.ho * es, 0, p.chunk, p.chunks, p.row_blocks, nullptr, nullptr};
+    a.part_stat = (float2*)ws;
+    a.part_o = (float*)ws + 2 * (size_t)p.chunks * d.total_q * d.heads;
+    return d.dtype == SGPRS_BF16 ? launch_typed<SGPRS_BF16>(a, p.decode, stream) : launch_typed<SGPRS_F32>(a, p.decode, stream);
 }
 
 }  // namespace sgprs
