@@ -31,6 +31,7 @@ struct AttentionArgs {
     long long hq, hk, hv, ho;        // bytes
     int slots;                       // query tiles, with room for each sequence's last one
     int chunk, chunks;               // keys that a workgroup takes of a sequence; of the longest one
+    int tile_rows;                   // of a prompt's tile, 0 for single tokens
     int row_blocks;                  // of 32 rows (queries x heads of a key head)
     float* part_o;                   // [chunk][token][head][head_dim], weights relative to part_stat
     float2* part_stat;               // [chunk][token][head]: maximum, sum
@@ -321,24 +322,45 @@ __device__ __forceinline__ void range_of(const int* offsets, int seq, int total,
 }
 #endif
 
+#if __HIP_DEVICE_COMPILE__
+// The last sequence s of n with key(offsets[s], s) <= value, for keys that do not fall: 64 of them are looked at at once.
+template <class Key> __device__ __forceinline__ int last_not_above(const int* offsets, int n, int value, Key key)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) >> 6, at = min(lo + lane * step, hi - 1);
+        const int below = (int)__popcll(__ballot(lo + lane * step < hi && key(offsets[at], at) <= value));
+        const int to = max(below - 1, 0);
+        hi = min(hi, lo + (to + 1) * step);
+        lo += to * step;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+#endif
+
 // Sequence and tile of a slot: a sequence's tiles start at slot q_offsets[s] / BM + s, which leaves each its own.
 __device__ __forceinline__ bool tile_of_slot(const AttentionArgs& a, int slot, int bm, int* seq, int* row, int* q0, int* nq)
 {
 #if __HIP_DEVICE_COMPILE__
-    int lo = 0, hi = a.n_seqs;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.q_offsets[mid] / bm + mid <= slot) lo = mid;
-        else hi = mid;
-    }
-    *seq = __builtin_amdgcn_readfirstlane(lo);
+    *seq = last_not_above(a.q_offsets, a.n_seqs, slot, [=](int offset, int s) { return offset / bm + s; });
     range_of(a.q_offsets, *seq, a.total_q, q0, nq);
     const int tile = __builtin_amdgcn_readfirstlane(slot - (a.q_offsets[*seq] / bm + *seq));
     *row = tile * bm;
-    return tile >= 0 && tile < (1 << 24) && *row < *nq;
+    return tile >= 0 && tile < (1 << 23) && *row < *nq;
 #else
     return false;
 #endif
+}
+
+constexpr int kPromptRows = 128;
+// Chunks of keys that the queries of one workgroup were split into; one: the result was written at once.  (tile_rows:
+// queries of a prompt's tile; 0 for single tokens.)
+__device__ __forceinline__ int chunks_of(const AttentionArgs& a, int query, int nq, int nk)
+{
+    int keys = nk;
+    if (a.tile_rows && a.causal) keys = min(nk, min(query / a.tile_rows * a.tile_rows + a.tile_rows, nq) + nk - nq);
+    return min(a.chunks, max(1, (keys + a.chunk - 1) / a.chunk));
 }
 
 // ---- prompts -----------------------------------------------------------------------------------
@@ -347,13 +369,13 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (DT == SGPRS_F32 && 
 {
 #if __HIP_DEVICE_COMPILE__
     typedef KvTile<DT, HD> Tile;
-    constexpr int ES = Tile::ES, STEPS = HD * ES / 32, BM = 128, LPW = Tile::BYTES / 1024 / 4;
-    static_assert(2 * LPW <= 63, "vmcnt range");
+    constexpr int ES = Tile::ES, STEPS = HD * ES / 32, BM = kPromptRows;
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // heavy tiles (the last ones under the causal mask) first; heads that share keys on one die where there are eight of them
-    const int item = blockIdx.x, j = item % a.heads, slot = a.slots - 1 - item / a.heads;
+    const int item = blockIdx.x % (a.slots * a.heads), chunk = blockIdx.x / (a.slots * a.heads);
+    const int j = item % a.heads, slot = a.slots - 1 - item / a.heads;
     const int kv_head = j % a.kv_heads, head = kv_head * a.group + j / a.kv_heads;
     int seq, row0, q0, nq;
     if (!tile_of_slot(a, slot, BM, &seq, &row0, &q0, &nq)) return;
@@ -361,7 +383,9 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (DT == SGPRS_F32 && 
     range_of(a.kv_offsets, seq, a.total_kv, &k0, &nk);
     const int row = row0 + wave * 32 + (lane & 31);       // of the sequence
     const int last_row = min(row0 + BM, nq) - 1;
-    const int keys = a.causal ? max(0, min(nk, last_row + nk - nq + 1)) : nk;  // that anyone here sees
+    const int all_keys = a.causal ? max(0, min(nk, last_row + nk - nq + 1)) : nk;  // that anyone here sees
+    const int begin = chunk * a.chunk, keys = min(all_keys - begin, a.chunk);       // of this chunk
+    if (chunk > 0 && keys <= 0) return;
     const int my_row = min(row, nq - 1);
     const int first_unseen = a.causal ? min(nk, my_row + nk - nq + 1) : nk;
     const int wave_first = min(row0 + wave * 32, nq - 1);
@@ -376,11 +400,11 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (DT == SGPRS_F32 && 
         q[c] = (2 * c + h) * 16 < row_bytes ? *(const u32x4_t*)(qp + (2 * c + h) * 16) : u32x4_t{0, 0, 0, 0};
         q[c] ^= a.q_flip;
     }
-    const unsigned char* kp = a.k + (long long)k0 * a.ldk + kv_head * a.hk;
-    const unsigned char* vp = a.v + (long long)k0 * a.ldv + kv_head * a.hv;
+    const unsigned char* kp = a.k + (long long)(k0 + begin) * a.ldk + kv_head * a.hk;
+    const unsigned char* vp = a.v + (long long)(k0 + begin) * a.ldv + kv_head * a.hv;
     auto request = [&](int t) {
         unsigned char* to = smem + (t & 1) * 2 * Tile::BYTES;
-        const int rows = max(0, min(Tile::KEYS, nk - t * Tile::KEYS));
+        const int rows = max(0, min(Tile::KEYS, nk - begin - t * Tile::KEYS));
         request_tile<DT, HD, Tile::KEYS>(kp + (long long)t * Tile::KEYS * a.ldk, a.ldk, rows, row_bytes, to, wave, 4);
         request_tile<DT, HD, Tile::KEYS>(vp + (long long)t * Tile::KEYS * a.ldv, a.ldv, rows, row_bytes, to + Tile::BYTES, wave, 4);
     };
@@ -394,7 +418,7 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (DT == SGPRS_F32 && 
         __builtin_amdgcn_sched_barrier(0);
         if (t + 1 < tiles) request(t + 1);
         const unsigned at = (unsigned)((t & 1) * 2 * Tile::BYTES);
-        const int key0 = t * Tile::KEYS;
+        const int key0 = begin + t * Tile::KEYS;
         if (key0 < wave_any) {
             auto nothing = [] {};
             if (key0 + Tile::KEYS <= wave_all) run.template tile<Tile::KEYS / 32, false>(q, a.scale_log2, at, at + Tile::BYTES, key0, first_unseen, nothing, nothing);
@@ -405,6 +429,19 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (DT == SGPRS_F32 && 
     }
     if (row >= nq) return;
     const float sum = run.sum + other_half(run.sum);
+    if (all_keys > a.chunk) {
+        const long long at = ((long long)chunk * a.total_q + q0 + row) * a.heads + head;
+        if (h == 0) a.part_stat[at] = make_float2(run.top, sum);
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int c = d * 32 + (i >> 2) * 8 + h * 4;
+                if (c < a.head_dim)
+                    *(float4*)(a.part_o + at * a.head_dim + c) = make_float4(run.o[d][i], run.o[d][i + 1], run.o[d][i + 2], run.o[d][i + 3]);
+            }
+        return;
+    }
     const float inv = normaliser(sum, first_unseen > 0);
     unsigned char* op = a.o + (long long)(q0 + row) * a.ldo + head * a.ho;
 #pragma unroll
@@ -551,71 +588,80 @@ template <int DT, int HD> __global__ __launch_bounds__((DecodeShape<DT, HD>::NW 
 #endif
 }
 
-// Joins the chunks of sequences that have several: a workgroup per query and head, four channels a lane, eight
-// chunks at a time, added in a fixed order.
-constexpr int kMaxChunks = 512 + 2;  // of plan_attention, on the largest partition
-template <int DT> __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs a)
+// Joins the chunks of what has several: 256 / ROWS threads per query and head, four channels a lane, 8 / ROWS chunks at
+// a time, added in a fixed order.
+constexpr int kMaxChunks = 512 + 2, kMaxPromptChunks = 64;  // of plan_attention, on the largest partition
+template <int DT, int ROWS> __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs a)
 {
 #if __HIP_DEVICE_COMPILE__
-    __shared__ float weight[kMaxChunks + 8];
+    constexpr int THREADS = 256 / ROWS, GROUPS = THREADS / 32;
+    static_assert(ROWS == 1 || ROWS == 4, "a workgroup or a wavefront");
+    __shared__ float weights[ROWS][ROWS == 1 ? kMaxChunks : kMaxPromptChunks];
     __shared__ float stat[8];
     __shared__ float4 part[8][32];
-    const int tid = threadIdx.x, lane = tid & 31, group = tid >> 5;
-    const int token = blockIdx.x / a.heads, head = blockIdx.x - token * a.heads;
-    int seq = 0, hi = a.n_seqs;  // the last sequence that does not begin behind the token
-    while (hi - seq > 1) {
-        const int mid = (seq + hi) >> 1;
-        if (a.q_offsets[mid] <= token) seq = mid;
-        else hi = mid;
-    }
-    int k0, nk;
+    const int tid = threadIdx.x % THREADS, lane = tid & 31, group = tid >> 5;
+    const long long item = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS;
+    const int token = (int)(item / a.heads), head = (int)(item - (long long)token * a.heads);
+    if (token >= a.total_q) return;
+    const int seq = last_not_above(a.q_offsets, a.n_seqs, token, [](int offset, int) { return offset; });
+    int q0, nq, k0, nk;
+    range_of(a.q_offsets, seq, a.total_q, &q0, &nq);
     range_of(a.kv_offsets, seq, a.total_kv, &k0, &nk);
-    if (nk <= a.chunk) return;
-    const int n = min(a.chunks, (nk + a.chunk - 1) / a.chunk);
+    const int query = token - q0, n = query < 0 || query >= nq ? 1 : chunks_of(a, query, nq, nk);
+    if (n == 1) return;
     const long long step = (long long)a.total_q * a.heads;
+    float* weight = weights[threadIdx.x / THREADS];
+    auto meet = [] {
+        if constexpr (ROWS == 1) __syncthreads();
+        else __builtin_amdgcn_s_waitcnt(0xC07F);
+    };
     // maximum, weights and sum
     float top = -INFINITY, total = 0.f;
-    for (int s = tid; s < n; s += 256) top = fmaxf(top, a.part_stat[s * step + blockIdx.x].x);
+    for (int s = tid; s < n; s += THREADS) top = fmaxf(top, a.part_stat[s * step + item].x);
 #pragma unroll
     for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-    if ((tid & 63) == 0) stat[tid >> 6] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(stat[0], stat[1]), fmaxf(stat[2], stat[3]));
-    for (int s = tid; s < n; s += 256) {
-        const float2 st = a.part_stat[s * step + blockIdx.x];
+    if constexpr (ROWS == 1) {
+        if ((tid & 63) == 0) stat[tid >> 6] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(stat[0], stat[1]), fmaxf(stat[2], stat[3]));
+    }
+    for (int s = tid; s < n; s += THREADS) {
+        const float2 st = a.part_stat[s * step + item];
         const float w = st.x == top ? 1.f : __builtin_amdgcn_exp2f(st.x - top);
         weight[s] = w;
         total = __builtin_fmaf(st.y, w, total);
     }
 #pragma unroll
     for (int x = 32; x; x >>= 1) total += __shfl_xor(total, x);
-    if ((tid & 63) == 0) stat[4 + (tid >> 6)] = total;
-    __syncthreads();
-    total = (stat[4] + stat[5]) + (stat[6] + stat[7]);
+    if constexpr (ROWS == 1) {
+        if ((tid & 63) == 0) stat[4 + (tid >> 6)] = total;
+    }
+    meet();
+    if constexpr (ROWS == 1) total = (stat[4] + stat[5]) + (stat[6] + stat[7]);
     float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
     const int c = lane * 4;
     if (c < a.head_dim) {
-        const float* p = a.part_o + (long long)blockIdx.x * a.head_dim + c;
+        const float* p = a.part_o + item * a.head_dim + c;
 #pragma unroll 4
-        for (int s = group; s < n; s += 8) {
+        for (int s = group; s < n; s += GROUPS) {
             const float w = weight[s];
             const float4 o = *(const float4*)(p + s * step * a.head_dim);
             z = make_float4(__builtin_fmaf(o.x, w, z.x), __builtin_fmaf(o.y, w, z.y), __builtin_fmaf(o.z, w, z.z), __builtin_fmaf(o.w, w, z.w));
         }
     }
-    part[group][lane] = z;
-    __syncthreads();
+    float4(*parts)[32] = part + threadIdx.x / THREADS * GROUPS;
+    parts[group][lane] = z;
+    meet();
     if (group || c >= a.head_dim) return;
     float out[4] = {z.x, z.y, z.z, z.w};
 #pragma unroll
-    for (int g = 1; g < 8; ++g) {
-        const float4 t = part[g][lane];
+    for (int g = 1; g < GROUPS; ++g) {
+        const float4 t = parts[g][lane];
         out[0] += t.x;
         out[1] += t.y;
         out[2] += t.z;
         out[3] += t.w;
     }
-    const int query = token - a.q_offsets[seq], nq = a.q_offsets[seq + 1] - a.q_offsets[seq];
     const float inv = normaliser(total, (a.causal ? min(nk, query + nk - nq + 1) : nk) > 0);
 #pragma unroll
     for (int e = 0; e < 4; ++e) out[e] *= inv;
@@ -635,7 +681,15 @@ static AttentionPlan plan_attention(const sgprs_attention_desc_t& d, int cus)
     p.decode = d.max_q <= 32;
     p.chunk = std::max(1, d.max_kv);
     p.chunks = 1;
-    if (p.decode) {
+    if (!p.decode) {
+        // Where the tiles leave most of the partition idle, a tile's keys are split: 128 keys or more for a workgroup.
+        const double tiles = (d.total_q / (double)kPromptRows + 0.5 * d.n_seqs) * d.heads;
+        const int most = std::min({(int)(2 * cus / tiles), (d.max_kv + 127) / 128, kMaxPromptChunks});
+        if (most > 1) {
+            p.chunk = ((d.max_kv + most - 1) / most + 63) / 64 * 64;
+            p.chunks = (d.max_kv + p.chunk - 1) / p.chunk;
+        }
+    } else {
         p.row_blocks = (d.max_q * (d.heads / d.kv_heads) + 31) / 32;
         // Chunks of keys for a workgroup a CU, 128 keys (a tile for each wavefront) or more: 16 caches of 2048 tokens,
         // 32/8 heads of 128, take 31.6 us so, 32.9 with two and 34.9 with three (more partial sums to join); one cache
@@ -669,13 +723,17 @@ template <auto kernel> static int launch_sized(long long grid, int threads, int 
 template <int DT, int HD> static int launch_shape(AttentionArgs a, bool decode, hipStream_t stream)
 {
     if (!decode) {
-        a.slots = a.total_q / 128 + a.n_seqs;
-        return launch_sized<attention_prompt_kernel<DT, HD>>((long long)a.slots * a.heads, 256, 4 * KvTile<DT, HD>::BYTES, a, stream);
+        a.slots = a.total_q / kPromptRows + a.n_seqs;
+        a.tile_rows = kPromptRows;
+        if ((long long)a.slots * a.heads >= (1ll << 31)) return fail(SGPRS_ERR_UNSUPPORTED, "%d sequences of %d tokens and %d heads", a.n_seqs, a.total_q, a.heads);
+        const int rc = launch_sized<attention_prompt_kernel<DT, HD>>((long long)a.chunks * a.slots * a.heads, 256, 4 * KvTile<DT, HD>::BYTES, a, stream);
+        if (rc || a.chunks == 1) return rc;
+        return launch_sized<attention_join_kernel<DT, 4>>(((long long)a.total_q * a.heads + 3) / 4, 256, 0, a, stream);
     }
     typedef DecodeShape<DT, HD> Shape;
     const int rc = launch_sized<attention_decode_kernel<DT, HD>>((long long)a.chunks * a.n_seqs * a.row_blocks * a.kv_heads, Shape::NW * 64, Shape::LDS, a, stream);
     if (rc || a.chunks == 1) return rc;
-    return launch_sized<attention_join_kernel<DT>>((long long)a.total_q * a.heads, 256, 0, a, stream);
+    return launch_sized<attention_join_kernel<DT, 1>>((long long)a.total_q * a.heads, 256, 0, a, stream);
 }
 
 template <int DT> static int launch_typed(const AttentionArgs& a, bool decode, hipStream_t stream)
@@ -694,7 +752,7 @@ int launch_attention(const sgprs_attention_desc_t& d, const void* q, const void*
     AttentionArgs a = {(const unsigned char*)q, (const unsigned char*)k, (const unsigned char*)v, (unsigned char*)o, q_offsets, kv_offsets,
                              d.n_seqs, d.total_q, d.total_kv, d.heads, d.kv_heads, d.heads / d.kv_heads, d.head_dim, d.causal,
                              std::fabs(d.scale) * 1.4426950408889634f, d.scale >= 0.f ? 0u : d.dtype == SGPRS_BF16 ? 0x80008000u : 0x80000000u,
-                             (int)(d.ldq * es), (int)(d.ldk * es), (int)(d.ldv * es), (int)(d.ldo * es), d.hq * es, d.hk * es, d.hv * es, d.ho * es, 0, p.chunk, p.chunks, p.row_blocks, nullptr, nullptr};
+                             (int)(d.ldq * es), (int)(d.ldk * es), (int)(d.ldv * es), (int)(d.ldo * es), d.hq * es, d.hk * es, d.hv * es, d.ho * es, 0, p.chunk, p.chunks, 0, p.row_blocks, nullptr, nullptr};
     a.part_stat = (float2*)ws;
     a.part_o = (float*)ws + 2 * (size_t)p.chunks * d.total_q * d.heads;
     return d.dtype == SGPRS_BF16 ? launch_typed<SGPRS_BF16>(a, p.decode, stream) : launch_typed<SGPRS_F32>(a, p.decode, stream);
