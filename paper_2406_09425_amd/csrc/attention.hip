@@ -69,9 +69,9 @@ template <int DT, int HD, int KEYS> __device__ __forceinline__ void request_tile
 {
     typedef KvTile<DT, HD> Tile;
     constexpr int RPI = 1024 / Tile::ROW, LOADS = KEYS * Tile::ROW / 1024;  // rows of a load
-    int lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(lane));  // the offsets are worked out in every tile rather than kept in registers
-    const int lrow = lane / Tile::CHUNKS, slot = (lane % Tile::CHUNKS) ^ Tile::swizzle(lrow);
+    unsigned lane = threadIdx.x & 63;
+    if constexpr (HD > 32) asm volatile("" : "+v"(lane));  // the offsets are worked out in every tile rather than kept in registers
+    const int lrow = (int)(lane / Tile::CHUNKS), slot = (int)(lane % Tile::CHUNKS) ^ Tile::swizzle(lrow);
     const int size = __builtin_amdgcn_readfirstlane(rows > 0 ? (rows - 1) * ld + row_bytes : 0);  // (a clamp is vector arithmetic)
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, size, 0x00020000);
     const unsigned first = (unsigned)(lrow * ld);
@@ -107,23 +107,31 @@ template <int DT, int HD> struct LanePlaces {
     static __device__ __forceinline__ unsigned plus(unsigned base, int r, int chunk) { return (base ^ (unsigned)((chunk ^ Tile::swizzle(r)) << 4)) + (unsigned)(r * Tile::ROW); }
 };
 
-// scores of 32 keys (rows `block` * 32 and on of a tile) with this lane's query
-template <int DT, int HD> __device__ __forceinline__ f32x16_t scores(unsigned k_base, int block, const u32x4_t* q)
+// Scores of BLOCKS blocks of 32 keys with this lane's query.  Two blocks' chains of MFMAs alternate; their first ones are
+// inline assembly for the constant 0 as addend (the compiler would clear 32 registers), and the one behind them hides
+// that from the second.
+template <int DT, int HD, int BLOCKS> __device__ __forceinline__ void scores(unsigned k_base, const u32x4_t* q, f32x16_t* s)
 {
     typedef KvTile<DT, HD> Tile;
     constexpr int STEPS = HD * Tile::ES / 32;  // two chunks each
-    f32x16_t s = {};
 #pragma unroll
-    for (int c = 0; c < STEPS; ++c) {
-        const u32x4_t k = *(const lds_u32x4_t*)(unsigned long)LanePlaces<DT, HD>::plus(k_base, block * 32, 2 * c);
-        if constexpr (DT == SGPRS_BF16) {
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, q[c]), s, 0, 0, 0);
-        } else {
+    for (int c = 0; c < STEPS; ++c)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[e]), __uint_as_float(q[c][e]), s, 0, 0, 0);
+        for (int b = 0; b < BLOCKS; ++b) {
+            const u32x4_t k = *(const lds_u32x4_t*)(unsigned long)LanePlaces<DT, HD>::plus(k_base, b * 32, 2 * c);
+            if constexpr (DT == SGPRS_BF16) {
+                if (BLOCKS == 2 && c == 0) {
+                    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s[b]) : "v"(k), "v"(q[c]));
+                } else {
+                    if (c == 0) s[b] = f32x16_t{};
+                    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, q[c]), s[b], 0, 0, 0);
+                }
+            } else {
+                if (c == 0) s[b] = f32x16_t{};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[e]), __uint_as_float(q[c][e]), s[b], 0, 0, 0);
+            }
         }
-    }
-    return s;
 }
 
 // v of channels 32 d and on at keys 16 u of a block, as the row operand (bf16)
@@ -238,7 +246,7 @@ template <int DT, int HD> __device__ __forceinline__ void add_not_finite(f32x16_
 template <int DT, int HD> struct Running {
     static constexpr int DB = HD / 32;
     f32x16_t o[DB];
-    float top, sum;
+    float top, sum;  // sum: of this half's keys
     LanePlaces<DT, HD> place;
     __device__ __forceinline__ void start()
     {
@@ -247,6 +255,7 @@ template <int DT, int HD> struct Running {
 #pragma unroll
         for (int d = 0; d < DB; ++d) o[d] = f32x16_t{};
     }
+    __device__ __forceinline__ float total() const { return sum + other_half(sum); }
     // BLOCKS blocks of 32 keys from key0 on, in LDS at k_at and v_at; keys from first_unseen on are not seen.  k_done
     // is called when k has been read, v_ready before v is.
     template <int BLOCKS, bool MASKED, class KDone, class VReady>
@@ -254,8 +263,7 @@ template <int DT, int HD> struct Running {
     {
         const unsigned k_base = place.hidden(place.k + k_at), v_base = place.hidden(place.v + v_at);
         f32x16_t s[BLOCKS];
-#pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) s[b] = scores<DT, HD>(k_base, b, q);
+        scores<DT, HD, BLOCKS>(k_base, q, s);
         k_done();
         const int mine = MASKED ? keys_left(key0, first_unseen) : 0;
         float most = -INFINITY;
@@ -364,12 +372,17 @@ __device__ __forceinline__ int chunks_of(const AttentionArgs& a, int query, int 
 }
 
 // ---- prompts -----------------------------------------------------------------------------------
-// 128 queries of one head per workgroup, 32 per wavefront; tiles of keys double buffered in LDS.
-template <int DT, int HD> __global__ __launch_bounds__(256, (DT == SGPRS_F32 && HD > 64 ? 1 : 2)) void attention_prompt_kernel(const AttentionArgs a)
+// 128 queries of one head per workgroup, 32 per wavefront; tiles of keys in an LDS ring of two or three stages.
+template <int DT, int HD> struct PromptShape {
+    static constexpr int STAGE = 2 * KvTile<DT, HD>::BYTES, STAGES = STAGE <= 16384 ? 3 : 2;
+};
+template <int DT, int HD> __global__ __launch_bounds__(256, (DT == SGPRS_F32 && HD > 64 ? 1 : DT == SGPRS_BF16 && HD <= 64 ? 3 : 2)) void attention_prompt_kernel(const AttentionArgs a)
 {
 #if __HIP_DEVICE_COMPILE__
     typedef KvTile<DT, HD> Tile;
     constexpr int ES = Tile::ES, STEPS = HD * ES / 32, BM = kPromptRows;
+    typedef PromptShape<DT, HD> Shape;
+    constexpr int NS = Shape::STAGES, LOADS = Shape::STAGE / 1024 / 4;  // of a wavefront for a tile
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -403,21 +416,23 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (DT == SGPRS_F32 && 
     const unsigned char* kp = a.k + (long long)(k0 + begin) * a.ldk + kv_head * a.hk;
     const unsigned char* vp = a.v + (long long)(k0 + begin) * a.ldv + kv_head * a.hv;
     auto request = [&](int t) {
-        unsigned char* to = smem + (t & 1) * 2 * Tile::BYTES;
-        const int rows = max(0, min(Tile::KEYS, nk - begin - t * Tile::KEYS));
+        unsigned char* to = smem + t % NS * Shape::STAGE;
+        const int rows = max(0, min(Tile::KEYS, nk - begin - t * Tile::KEYS));  // (none behind the last tile)
         request_tile<DT, HD, Tile::KEYS>(kp + (long long)t * Tile::KEYS * a.ldk, a.ldk, rows, row_bytes, to, wave, 4);
         request_tile<DT, HD, Tile::KEYS>(vp + (long long)t * Tile::KEYS * a.ldv, a.ldv, rows, row_bytes, to + Tile::BYTES, wave, 4);
     };
     Running<DT, HD> run;
     run.start();
     const int tiles = (keys + Tile::KEYS - 1) / Tile::KEYS;
-    if (tiles > 0) request(0);
+#pragma unroll
+    for (int t = 0; t < NS - 1; ++t) request(t);
     for (int t = 0; t < tiles; ++t) {
-        __builtin_amdgcn_s_waitcnt(0x0F70);  // this tile has landed
-        __builtin_amdgcn_s_barrier();        // everyone's, and everyone has left the other buffer
+        constexpr int BEHIND = (NS - 2) * LOADS;
+        __builtin_amdgcn_s_waitcnt((BEHIND & 15) | ((BEHIND >> 4) << 14) | 0x0F70);  // this tile has landed
+        __builtin_amdgcn_s_barrier();  // everyone's, and everyone has left the buffer of the tile before
         __builtin_amdgcn_sched_barrier(0);
-        if (t + 1 < tiles) request(t + 1);
-        const unsigned at = (unsigned)((t & 1) * 2 * Tile::BYTES);
+        request(t + NS - 1);
+        const unsigned at = (unsigned)(t % NS * Shape::STAGE);
         const int key0 = begin + t * Tile::KEYS;
         if (key0 < wave_any) {
             auto nothing = [] {};
@@ -427,8 +442,9 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (DT == SGPRS_F32 && 
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0xC07F);
     }
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // requests behind the last tile write zeros
     if (row >= nq) return;
-    const float sum = run.sum + other_half(run.sum);
+    const float sum = run.total();
     if (all_keys > a.chunk) {
         const long long at = ((long long)chunk * a.total_q + q0 + row) * a.heads + head;
         if (h == 0) a.part_stat[at] = make_float2(run.top, sum);
@@ -553,7 +569,7 @@ template <int DT, int HD> __global__ __launch_bounds__((DecodeShape<DT, HD>::NW 
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
             *(float4*)(sums + (wave * 32 + col) * Shape::SROW + d * 32 + (i >> 2) * 8 + h * 4) = make_float4(run.o[d][i], run.o[d][i + 1], run.o[d][i + 2], run.o[d][i + 3]);
-    const float sum = run.sum + other_half(run.sum);
+    const float sum = run.total();
     if (h == 0) {
         tops[wave * 32 + col] = run.top;
         totals[wave * 32 + col] = sum;
@@ -726,7 +742,7 @@ template <int DT, int HD> static int launch_shape(AttentionArgs a, bool decode, 
         a.slots = a.total_q / kPromptRows + a.n_seqs;
         a.tile_rows = kPromptRows;
         if ((long long)a.slots * a.heads >= (1ll << 31)) return fail(SGPRS_ERR_UNSUPPORTED, "%d sequences of %d tokens and %d heads", a.n_seqs, a.total_q, a.heads);
-        const int rc = launch_sized<attention_prompt_kernel<DT, HD>>((long long)a.chunks * a.slots * a.heads, 256, 4 * KvTile<DT, HD>::BYTES, a, stream);
+        const int rc = launch_sized<attention_prompt_kernel<DT, HD>>((long long)a.chunks * a.slots * a.heads, 256, PromptShape<DT, HD>::STAGES * PromptShape<DT, HD>::STAGE, a, stream);
         if (rc || a.chunks == 1) return rc;
         return launch_sized<attention_join_kernel<DT, 4>>(((long long)a.total_q * a.heads + 3) / 4, 256, 0, a, stream);
     }
