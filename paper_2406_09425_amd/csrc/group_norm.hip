@@ -9,6 +9,7 @@
 //     workspace) and one that merges an image's chunks and writes the results;
 //   * a norm over all channels of single positions (layer norm) is a wavefront per row.
 #include <algorithm>
+#include <type_traits>
 
 #include "block_ops.h"
 
@@ -31,6 +32,7 @@ struct NormArgs {
     unsigned vec_mul;
     int vec_sh;              // thread / vectors
     int slice_groups;
+    int share_log2;          // lanes that add up a group
     int chunks;              // of an image's positions
 };
 
@@ -115,14 +117,31 @@ __device__ __forceinline__ void finish_vector(const NormArgs& a, const u32x4_t& 
     N::store(y, N::pack(o), live);
 }
 
+// Sum over `share` neighbouring lanes (a power of two up to 64), in all of them.  Within 16 lanes by data-parallel
+// moves: neighbours, pairs, then mirrored halves, which hold the same sums as the lanes beside them.
+__device__ __forceinline__ float lanes_sum(float v, int share)
+{
+#if __HIP_DEVICE_COMPILE__
+    auto moved = [](float x, auto control) {
+        return __uint_as_float((unsigned)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), decltype(control)::value, 0xf, 0xf, true));
+    };
+    if (share > 1) v += moved(v, std::integral_constant<int, 0xB1>());   // quad_perm 1 0 3 2
+    if (share > 2) v += moved(v, std::integral_constant<int, 0x4E>());   // quad_perm 2 3 0 1
+    if (share > 4) v += moved(v, std::integral_constant<int, 0x141>());  // row_half_mirror
+    if (share > 8) v += moved(v, std::integral_constant<int, 0x140>());  // row_mirror
+    if (share > 16) v += __shfl_xor(v, 16);
+    if (share > 32) v += __shfl_xor(v, 32);
+#endif
+    return v;
+}
+
 // Sums over a workgroup, group by group: thread (s, v) brings V values of vector v (zeros for channels that do
-// not exist and threads that have none); total[g] gets the sum of group g of the slice.  scratch: a float for
-// every value, and one for every thread.  All threads call it; the order is fixed.
+// not exist); total[g] gets the sum of group g of the slice.  scratch: a float for every value.  All threads call it;
+// `share` neighbouring lanes add up a group, in a fixed order.
 template <int V>
 __device__ __forceinline__ void group_sums(const NormArgs& a, const float* value, int groups, float* scratch, float* total)
 {
     const int tid = threadIdx.x, T = blockDim.x;
-    float* parts = scratch + T * V;
     const bool whole = a.per % V == 0;  // a vector lies within one group
     if (whole) {
         float s = value[0];
@@ -135,25 +154,28 @@ __device__ __forceinline__ void group_sums(const NormArgs& a, const float* value
     }
     __syncthreads();
     const int row = whole ? a.vectors : a.vectors * V, width = whole ? a.per / V : a.per;  // of a position's values, of a group's
-    for (int g0 = 0; g0 < groups; g0 += T) {  // more groups than threads: in rounds
-        const int now = min(groups - g0, T), share = T / now;
-        const int g = tid % now, part = tid / now;
-        if (part < share) {
-            float s = 0.f;
-            const int at = (g0 + g) * width;
-            for (int p = part; p < a.step; p += share)
-                for (int i = 0; i < width; ++i) s += scratch[p * row + at + i];
-            parts[part * now + g] = s;
+    const int share = 1 << a.share_log2, part = tid & (share - 1);
+    for (int g0 = 0; g0 < groups; g0 += T >> a.share_log2) {
+        const int g = g0 + (tid >> a.share_log2);
+        float s = 0.f;
+        if (g < groups) {
+            const float* at = scratch + g * width;
+            if (width == 1) {
+#pragma unroll 4
+                for (int p = part; p < a.step; p += share) s += at[p * row];
+            } else if (width == 2) {
+#pragma unroll 4
+                for (int p = part; p < a.step; p += share) s += at[p * row] + at[p * row + 1];
+            } else {
+                for (int p = part; p < a.step; p += share)
+#pragma unroll 4
+                    for (int i = 0; i < width; ++i) s += at[p * row + i];
+            }
         }
-        __syncthreads();
-        if (tid < now) {
-            float s = 0.f;
-            const int used = min(share, a.step);
-            for (int p = 0; p < used; ++p) s += parts[p * now + tid];
-            total[g0 + tid] = s;
-        }
-        __syncthreads();
+        s = lanes_sum(s, share);
+        if (g < groups && part == 0) total[g] = s;
     }
+    __syncthreads();
 }
 
 // A workgroup's share: positions `first` and on of an image, channels c0 and on; a thread's vector and first position.
@@ -197,10 +219,11 @@ template <int DT, int ACT, bool WHOLE, int NV, bool FUSED> __global__ __launch_b
     extern __shared__ __align__(16) float lds[];
     const int tid = threadIdx.x, T = blockDim.x;
     const NormShare<DT, WHOLE, NV> m(a);
-    float* total = lds + T * (V + 1);  // per group of the slice
-    u32x4_t x[NV], r[FUSED ? NV : 1];
+    float* total = lds + T * V;  // per group of the slice
+    constexpr bool EARLY = FUSED && NV < 8;  // the residual is requested with x where there are registers for it
+    u32x4_t x[NV], r[EARLY ? NV : 1];
     m.load(a, a.x, a.ldx, x);
-    if constexpr (FUSED) {
+    if constexpr (EARLY) {
         if (a.residual) m.load(a, a.residual, a.ldr, r);
     }
     float gamma[V], beta[V];
@@ -215,7 +238,7 @@ template <int DT, int ACT, bool WHOLE, int NV, bool FUSED> __global__ __launch_b
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int e = 0; e < V; ++e) sum[e] += m.has(a, k) ? N::get(x[k], e) : 0.f;
+        for (int e = 0; e < V; ++e) sum[e] = __builtin_fmaf(N::get(x[k], e), m.has(a, k) ? 1.f : 0.f, sum[e]);  // (what a load repeats is of the same group)
     group_sums<V>(a, sum, m.groups, lds, total);
     const float inv_count = 1.f / ((float)m.rows * (float)a.per);
     int group[V];
@@ -229,7 +252,7 @@ template <int DT, int ACT, bool WHOLE, int NV, bool FUSED> __global__ __launch_b
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float t = N::get(x[k], e) - mean[e];
-            sq[e] += (WHOLE || e < m.live) && m.has(a, k) ? t * t : 0.f;
+            sq[e] = __builtin_fmaf((WHOLE || e < m.live) && m.has(a, k) ? t : 0.f, t, sq[e]);
         }
     float2* partial = a.partial + ((long long)m.image * a.chunks + blockIdx.y) * a.groups + blockIdx.x * a.slice_groups;
     if constexpr (!FUSED) {
@@ -241,11 +264,17 @@ template <int DT, int ACT, bool WHOLE, int NV, bool FUSED> __global__ __launch_b
         for (int g = tid; g < m.groups; g += T) partial[g].y = total[g];
     } else if (m.live > 0) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) gamma[e] *= 1.f / sqrtf(total[group[e]] * inv_count + a.eps);
+        for (int e = 0; e < V; ++e) gamma[e] *= __builtin_amdgcn_rsqf(total[group[e]] * inv_count + a.eps);
         unsigned char* yp = a.y + m.row0 * a.ldy + (long long)c * N::ES;
+        const unsigned char* rp = a.residual + m.row0 * a.ldr + (long long)c * N::ES;
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (m.has(a, k)) finish_vector<DT, ACT, WHOLE>(a, x[k], r[k], mean, gamma, beta, yp + (m.s + k * a.step) * a.ldy, m.live);
+        for (int k = 0; k < NV; ++k) {
+            if (!m.has(a, k)) continue;
+            if constexpr (!EARLY) {
+                if (a.residual) r[0] = N::load(rp + (m.s + k * a.step) * a.ldr, m.live);
+            }
+            finish_vector<DT, ACT, WHOLE>(a, x[k], r[EARLY ? k : 0], mean, gamma, beta, yp + (m.s + k * a.step) * a.ldy, m.live);
+        }
     }
 }
 
@@ -265,40 +294,28 @@ template <int DT, int ACT, bool WHOLE, int NV> __global__ __launch_bounds__(1024
     const int c = m.c0 + (m.live > 0 ? m.v * V : 0);
     N::per_channel(a.gamma ? a.gamma + c : nullptr, m.live, 1.f, gamma);
     N::per_channel(a.beta ? a.beta + c : nullptr, m.live, 0.f, beta);
-    // Chunks of a group: `share` threads, then their results in order.  All chunks but the last count `full` positions.
+    // Chunks of a group: `share` neighbouring lanes, in order.  All chunks but the last count `full` positions.
     const float2* partial = a.partial + (long long)m.image * a.chunks * a.groups + blockIdx.x * a.slice_groups;
-    float *parts = lds, *means = lds + T, *scales = means + groups;
+    float *means = lds, *scales = means + groups;
     const float inv_hw = 1.f / (float)a.hw;
     const int last = a.hw - (a.chunks - 1) * full;
-    for (int g0 = 0; g0 < groups; g0 += T) {
-        const int now = min(groups - g0, T), share = T / now, g = tid % now, part = tid / now;
-        const bool in = part < share;
-        const int used = min(share, a.chunks);
-        float t = 0.f;
-        if (in)
-            for (int k = part; k < a.chunks; k += share) t += partial[(long long)k * a.groups + g0 + g].x * (float)(k == a.chunks - 1 ? last : full);
-        __syncthreads();
-        if (in) parts[part * now + g] = t;
-        __syncthreads();
-        float mean = 0.f;
-        if (in) {
-            for (int p = 0; p < used; ++p) mean += parts[p * now + g];
-            mean *= inv_hw;
+    const int share = 1 << a.share_log2, part = tid & (share - 1);
+    for (int g0 = 0; g0 < groups; g0 += T >> a.share_log2) {
+        const int g = g0 + (tid >> a.share_log2);
+        const float2* from = partial + min(g, groups - 1);
+        float mean = 0.f, m2 = 0.f;
+#pragma unroll 4
+        for (int k = part; k < a.chunks; k += share) mean += from[(long long)k * a.groups].x * (float)(k == a.chunks - 1 ? last : full);
+        mean = lanes_sum(mean, share) * inv_hw;
+#pragma unroll 4
+        for (int k = part; k < a.chunks; k += share) {
+            const float2 one = from[(long long)k * a.groups];
+            m2 += one.y + (one.x - mean) * (one.x - mean) * ((float)(k == a.chunks - 1 ? last : full) * (float)a.per);
         }
-        t = 0.f;
-        if (in)
-            for (int k = part; k < a.chunks; k += share) {
-                const float2 one = partial[(long long)k * a.groups + g0 + g];
-                t += one.y + (one.x - mean) * (one.x - mean) * ((float)(k == a.chunks - 1 ? last : full) * (float)a.per);
-            }
-        __syncthreads();
-        if (in) parts[part * now + g] = t;
-        __syncthreads();
-        if (tid < now) {
-            float m2 = 0.f;
-            for (int p = 0; p < used; ++p) m2 += parts[p * now + g];
-            means[g0 + tid] = mean;
-            scales[g0 + tid] = 1.f / sqrtf(m2 * inv_hw / (float)a.per + a.eps);
+        m2 = lanes_sum(m2, share);
+        if (g < groups && part == 0) {
+            means[g] = mean;
+            scales[g] = __builtin_amdgcn_rsqf(m2 * inv_hw / (float)a.per + a.eps);
         }
     }
     __syncthreads();
@@ -313,13 +330,6 @@ template <int DT, int ACT, bool WHOLE, int NV> __global__ __launch_bounds__(1024
 #pragma unroll
     for (int k = 0; k < NV; ++k)
         if (m.has(a, k)) finish_vector<DT, ACT, WHOLE>(a, x[k], r[k], mean, gamma, beta, yp + (m.s + k * a.step) * a.ldy, m.live);
-}
-
-__device__ __forceinline__ float wave_sum(float v)
-{
-#pragma unroll
-    for (int s = 32; s; s >>= 1) v += __shfl_xor(v, s);
-    return v;
 }
 
 // One group over single positions: a wavefront per row, NV vectors a lane, the next row requested before this one's sums.
@@ -363,7 +373,7 @@ template <int DT, int ACT, bool WHOLE, int NV> __global__ __launch_bounds__(256)
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < V; ++e) sum += live[k] ? N::get(x[k], e) : 0.f;
-        const float mean1 = wave_sum(sum) * inv_c;
+        const float mean1 = lanes_sum(sum, 64) * inv_c;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -371,7 +381,7 @@ template <int DT, int ACT, bool WHOLE, int NV> __global__ __launch_bounds__(256)
                 const float t = N::get(x[k], e) - mean1;
                 sq += (WHOLE ? live[k] > 0 : e < live[k]) ? t * t : 0.f;
             }
-        const float inv = 1.f / sqrtf(wave_sum(sq) * inv_c + a.eps);
+        const float inv = __builtin_amdgcn_rsqf(lanes_sum(sq, 64) * inv_c + a.eps);
         float mean[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) mean[e] = mean1;
@@ -439,7 +449,7 @@ static NormPlan plan_norm(const sgprs_group_norm_desc_t& d, int cus)
         p.nv = 1;
         while (p.nv < 8 && !holds(p.threads, p.nv)) p.nv *= 2;
     } else {
-        p.threads = p.vectors > 512 ? 1024 : 512;
+        p.threads = p.vectors > 512 ? 1024 : p.vectors > 256 ? 512 : 256;
         p.nv = 8;
     }
     p.step = std::max(1, p.threads / p.vectors);
@@ -466,7 +476,7 @@ template <int DT, int ACT, bool WHOLE> static int launch_norm(const NormArgs& a,
         }
     } else {
         const dim3 grid(p.slices, p.chunks, a.n);
-        const size_t lds = sizeof(float) * ((size_t)p.threads * (V + 1) + 2 * a.slice_groups);
+        const size_t lds = sizeof(float) * ((size_t)p.threads * V + 2 * a.slice_groups);
         if (p.fused) {
             switch (p.nv) {
             case 1: SGPRS_LAUNCH((group_norm_chunk_kernel<DT, ACT, WHOLE, 1, true>), grid, p.threads, lds, stream, a); break;
@@ -501,11 +511,12 @@ int launch_group_norm(const sgprs_group_norm_desc_t& d, const void* x, const flo
     const long long es = (long long)dtype_size(d.dtype);
     const int V = 16 / (int)es;
     NormArgs a = {(const unsigned char*)x, gamma, beta, (const unsigned char*)residual, (unsigned char*)y, (float2*)ws, d.n, d.hw, d.c, d.groups,
-                  d.c / d.groups, 0, 0, d.ldx * es, d.ldr * es, d.ldy * es, d.eps, p.slice, p.vectors, p.step, 0, 0, 0, p.chunks};
+                  d.c / d.groups, 0, 0, d.ldx * es, d.ldr * es, d.ldy * es, d.eps, p.slice, p.vectors, p.step, 0, 0, 0, 0, p.chunks};
     div_constants(a.per, &a.per_mul, &a.per_sh);
     if (!p.rows) {
         div_constants(p.vectors, &a.vec_mul, &a.vec_sh);
         a.slice_groups = p.slice / a.per;
+        while (a.share_log2 < 6 && (2 << a.share_log2) * a.slice_groups <= p.threads) ++a.share_log2;
     }
     const bool whole = d.c % V == 0 && (p.rows || p.slice % V == 0);
     if (d.dtype == SGPRS_BF16)
