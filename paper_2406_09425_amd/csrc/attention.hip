@@ -9,6 +9,7 @@
 // touching.  Weights are taken relative to 2^8 times the maximum, so that none is above 1.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 #include "block_ops.h"
 
@@ -107,31 +108,49 @@ template <int DT, int HD> struct LanePlaces {
     static __device__ __forceinline__ unsigned plus(unsigned base, int r, int chunk) { return (base ^ (unsigned)((chunk ^ Tile::swizzle(r)) << 4)) + (unsigned)(r * Tile::ROW); }
 };
 
-// Scores of BLOCKS blocks of 32 keys with this lane's query.  Two blocks' chains of MFMAs alternate; their first ones are
-// inline assembly for the constant 0 as addend (the compiler would clear 32 registers), and the one behind them hides
-// that from the second.
+// Scores of BLOCKS blocks of 32 keys with this lane's query, as two chains of MFMAs that alternate: the two blocks', or
+// one block's even and odd steps.  Two blocks' first MFMAs are inline assembly for the constant 0 as addend (the compiler
+// would clear 32 registers); their results are first used two MFMAs on.
 template <int DT, int HD, int BLOCKS> __device__ __forceinline__ void scores(unsigned k_base, const u32x4_t* q, f32x16_t* s)
 {
     typedef KvTile<DT, HD> Tile;
     constexpr int STEPS = HD * Tile::ES / 32;  // two chunks each
+    auto chunk = [&](int b, int c) { return *(const lds_u32x4_t*)(unsigned long)LanePlaces<DT, HD>::plus(k_base, b * 32, 2 * c); };
+    auto add = [&](f32x16_t& sum, u32x4_t k, int c) {
+        if constexpr (DT == SGPRS_BF16) {
+            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, q[c]), sum, 0, 0, 0);
+        } else {
 #pragma unroll
-    for (int c = 0; c < STEPS; ++c)
+            for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[e]), __uint_as_float(q[c][e]), sum, 0, 0, 0);
+        }
+    };
+    if constexpr (BLOCKS == 2) {
+        static_assert(DT == SGPRS_BF16, "the assembly's type");
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) {
-            const u32x4_t k = *(const lds_u32x4_t*)(unsigned long)LanePlaces<DT, HD>::plus(k_base, b * 32, 2 * c);
+        for (int c = 0; c < STEPS; ++c)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const u32x4_t k = chunk(b, c);
+                if (c == 0) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s[b]) : "v"(k), "v"(q[c]));
+                else add(s[b], k, c);
+            }
+    } else {
+        f32x16_t even = {}, odd = {};
+#pragma unroll
+        for (int c = 0; c < STEPS; ++c) {
+            const u32x4_t k = chunk(0, c);
             if constexpr (DT == SGPRS_BF16) {
-                if (BLOCKS == 2 && c == 0) {
-                    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s[b]) : "v"(k), "v"(q[c]));
-                } else {
-                    if (c == 0) s[b] = f32x16_t{};
-                    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, q[c]), s[b], 0, 0, 0);
-                }
+                add(c % 2 ? odd : even, k, c);
             } else {
-                if (c == 0) s[b] = f32x16_t{};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[e]), __uint_as_float(q[c][e]), s[b], 0, 0, 0);
+                for (int e = 0; e < 4; ++e) {
+                    f32x16_t& sum = e % 2 ? odd : even;
+                    sum = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[e]), __uint_as_float(q[c][e]), sum, 0, 0, 0);
+                }
             }
         }
+        s[0] = even + odd;
+    }
 }
 
 // v of channels 32 d and on at keys 16 u of a block, as the row operand (bf16)
@@ -299,9 +318,9 @@ template <int DT, int HD> struct Running {
             }
             add_values<DT, HD, MASKED>(o, p, v_base, b, &odd);
         }
-        if (MASKED && __any(odd)) {
-#pragma unroll 1
-            for (int b = 0; b < BLOCKS; ++b) add_not_finite<DT, HD>(o, v_base, b, key0, first_unseen);
+        if constexpr (MASKED) {
+            static_assert(BLOCKS == 1, "a block at a time");
+            if (__any(odd)) add_not_finite<DT, HD>(o, v_base, 0, key0, first_unseen);
         }
     }
 };
@@ -436,8 +455,14 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (DT == SGPRS_F32 && 
         const int key0 = begin + t * Tile::KEYS;
         if (key0 < wave_any) {
             auto nothing = [] {};
-            if (key0 + Tile::KEYS <= wave_all) run.template tile<Tile::KEYS / 32, false>(q, a.scale_log2, at, at + Tile::BYTES, key0, first_unseen, nothing, nothing);
-            else run.template tile<Tile::KEYS / 32, true>(q, a.scale_log2, at, at + Tile::BYTES, key0, first_unseen, nothing, nothing);
+            const unsigned v_at = at + Tile::BYTES;
+            if (key0 + Tile::KEYS <= wave_all) {
+                run.template tile<Tile::KEYS / 32, false>(q, a.scale_log2, at, v_at, key0, first_unseen, nothing, nothing);
+            } else {  // block by block, those that somebody here sees
+#pragma unroll 1
+                for (int b = 0; b < Tile::KEYS && key0 + b < wave_any; b += 32)
+                    run.template tile<1, true>(q, a.scale_log2, at + b * Tile::ROW, v_at + b * Tile::ROW, key0 + b, first_unseen, nothing, nothing);
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0xC07F);
@@ -698,11 +723,23 @@ static AttentionPlan plan_attention(const sgprs_attention_desc_t& d, int cus)
     p.chunk = std::max(1, d.max_kv);
     p.chunks = 1;
     if (!p.decode) {
-        // Where the tiles leave most of the partition idle, a tile's keys are split: 128 keys or more for a workgroup.
+        // Where the tiles leave workgroup slots idle (one a CU for wide fp32 heads, else two), a tile's keys may be split,
+        // 128 or more for a workgroup; under the causal mask half of the chunks lie behind what their queries see.  Worth
+        // it where the estimate, in us, says so: a workgroup's keys one after another, against a second launch and partial
+        // sums written and read.  Split / whole, 256 CUs: 4096 causal tokens, 4 heads of 128, 57 / 112 us; 1000, 2 of 64,
+        // 13 / 22; ragged fp32, 6/2 of 72, 39 / 92; but 8 x 600, 8 of 128, 43 / 31; 2 x 1000, 8 of 64, 30 / 22.
         const double tiles = (d.total_q / (double)kPromptRows + 0.5 * d.n_seqs) * d.heads;
-        const int most = std::min({(int)(2 * cus / tiles), (d.max_kv + 127) / 128, kMaxPromptChunks});
-        if (most > 1) {
-            p.chunk = ((d.max_kv + most - 1) / most + 63) / 64 * 64;
+        const bool f32 = d.dtype == SGPRS_F32;
+        const double slots = (f32 && d.head_dim > 64 ? 1.0 : 2.0) * cus * (d.causal ? 2 : 1);
+        const int most = std::min({(int)std::lround(std::min(slots / tiles, 1000.0)), (d.max_kv + 127) / 128, kMaxPromptChunks});
+        const double keys_us = d.max_kv * (f32 ? 0.001 * d.head_dim : 0.006 + 0.00015 * d.head_dim);
+        const double chunk_us = 2.0 * 4 * d.total_q * d.heads * d.head_dim / 2.5e6;
+        auto us = [&](int c) { return keys_us / c + (c > 1 ? 6 + (d.causal ? 0.5 * (c + 1) : c) * chunk_us : 0.0); };
+        int best = 1;
+        for (int c = 2; c <= most; ++c)
+            if (us(c) < us(best)) best = c;
+        if (best > 1) {
+            p.chunk = ((d.max_kv + best - 1) / best + 63) / 64 * 64;
             p.chunks = (d.max_kv + p.chunk - 1) / p.chunk;
         }
     } else {
