@@ -289,7 +289,8 @@ template <int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM * BN >= 
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int r = 0; r < R; ++r) read_fragment(0, 0, r);
-    for (int t = 0; t < tiles; ++t) {
+    int t = 0;
+    do {  // (k > 0: without a loop that may not run, the accumulators are cleared in one place)
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -312,7 +313,7 @@ template <int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM * BN >= 
                 if (at % READ_EVERY == 0 && at / READ_EVERY < R) read_fragment(t + 1, 0, at / READ_EVERY);
                 __builtin_amdgcn_sched_barrier(0);
             }
-    }
+    } while (++t < tiles);
     settle(acc);
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();

@@ -139,6 +139,27 @@ def test_linear_on_partitions(pools, name, cus, shape):
 
 
 @pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("shape,cus", [((2816, 2800, 520), 128), ((2815, 2817, 512), 128), ((1500, 1400, 96), 64), ((1501, 1300, 101), 64)], ids=str)
+def test_linear_large_tiles(pools, name, shape, cus):
+    """Products whose tiles fill a partition: the largest tiles, ragged at both edges, with and without whole chunks."""
+    run_linear(pools, name, *shape, act=2, res=True, cus=cus, seed=1)
+
+
+@pytest.mark.parametrize("m,n,k,cus", [(300, 140, 96, 256), (600, 700, 40, 8)])
+def test_linear_fp32_at_the_ends_of_the_range(pools, m, n, k, cus):
+    """Values that round up to infinity in fewer bits, and values whose lower parts fall below the normal range."""
+    g = gen(10)
+    x, w = torch.randn(m, k, generator=g), torch.randn(n, k, generator=g)
+    x[3] = 0.0
+    x[3, 1] = 3.4028e38
+    w[:, 1] = w[:, 1].clamp(-0.9, 0.9)
+    x[40:70] *= 2.0 ** -118
+    x[100, :] = 2.0 ** -120
+    x[101, :] = 0.0
+    run_linear(pools, "f32", m, n, k, bias=False, x=x, w=w, cus=cus)
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
 @pytest.mark.parametrize("m", [7, 40, 300])
 def test_linear_in_place_residual(pools, name, m):
     run_linear(pools, name, m, 264, 512, res=True, inplace=True, pads=(0, 0, 8, 0), seed=m)
@@ -366,6 +387,27 @@ def test_attention_rows_without_keys(pools, name, causal, q_lens, kv_lens):
 
 
 @pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("q_lens,kv_lens", [([40, 1100], [40, 1100]), ([200, 33], [2100, 1500]), ([1000], [420]), ([140, 60, 1], [1300, 0, 1900])], ids=str)
+@pytest.mark.parametrize("heads,kv_heads,dim", [(2, 1, 128), (1, 1, 64)])
+def test_attention_prompts_split_by_keys(pools, name, causal, q_lens, kv_lens, heads, kv_heads, dim):
+    """Few tiles and many keys: a tile's keys go to several workgroups, some of which hold none that it sees."""
+    d = S.AttentionDesc(n_seqs=len(q_lens), total_q=sum(q_lens), total_kv=sum(kv_lens), max_q=max(q_lens), max_kv=max(kv_lens), heads=heads, kv_heads=kv_heads,
+                        head_dim=dim, dtype=DT[name][0], causal=int(causal))
+    if max(kv_lens) >= 1000:
+        assert S.sgprs_attention_workspace(d, CUS) > 0
+    run_attention(pools, name, q_lens, kv_lens, heads, kv_heads, dim, causal, seed=dim)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_attention_split_prompts_do_not_spread_what_is_not_finite(pools, bad):
+    def change(q, k, v):
+        v[700, :, 5] = bad
+
+    run_attention(pools, "bf16", [1200], [1200], 2, 1, 64, True, seed=3, change=change)
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
 @pytest.mark.parametrize("layout,pad", [("tokens", 8), ("tokens", 64), ("heads", 0), ("heads", 8)])
 @pytest.mark.parametrize("q_lens,kv_lens", [([1, 2], [300, 65]), ([90, 200], [90, 200])], ids=["tokens", "prompts"])
 def test_attention_layouts(pools, name, layout, pad, q_lens, kv_lens):
@@ -457,6 +499,41 @@ def test_attention_cache_beyond_32_bit_offsets(pools):
 
 
 # ---- all together --------------------------------------------------------------------------------
+def test_partitions_side_by_side():
+    """The same calls on two partitions of a pool at once, each with a workspace of its own, as one after the other."""
+    pool = S.Pool(2, 64)
+    try:
+        g = gen(41)
+        m, c, heads = 600, 128, 2
+        x, w = torch.randn(m, c, generator=g).bfloat16().cuda(), (torch.randn(3 * c, c, generator=g) / 11).bfloat16().cuda()
+        off = offsets([600])
+        dl = S.LinearDesc(m=m, n=3 * c, k=c, dtype=S.SGPRS_BF16)
+        da = S.AttentionDesc(n_seqs=1, total_q=m, total_kv=m, max_q=m, max_kv=m, heads=heads, kv_heads=heads, head_dim=c // heads, dtype=S.SGPRS_BF16,
+                             causal=1, ldq=3 * c, ldk=3 * c, ldv=3 * c)
+        dn = S.GroupNormDesc(n=1, hw=m, c=c, groups=4, dtype=S.SGPRS_BF16, eps=1e-5)
+        need = [f(d, 64) for f, d in ((S.sgprs_linear_workspace, dl), (S.sgprs_attention_workspace, da), (S.sgprs_group_norm_workspace, dn))]
+        state = [dict(rows=torch.zeros(m, 3 * c, dtype=torch.bfloat16, device="cuda"), mixed=torch.zeros_like(x), out=torch.zeros_like(x),
+                      ws=torch.empty(max(need + [16]), dtype=torch.uint8, device="cuda")) for _ in range(2)]
+        torch.cuda.synchronize()
+
+        def enqueue(p):
+            s = state[p]
+            S.sgprs_linear(dl, ptr(x), ptr(w), None, None, ptr(s["rows"]), ptr(s["ws"]), need[0], pool, p)
+            S.sgprs_attention(da, ptr(s["rows"]), ptr(s["rows"]) + 2 * c, ptr(s["rows"]) + 4 * c, ptr(off), ptr(off), ptr(s["mixed"]), ptr(s["ws"]), need[1], pool, p)
+            S.sgprs_group_norm(dn, ptr(s["mixed"]), None, None, ptr(x), ptr(s["out"]), ptr(s["ws"]), need[2], pool, p)
+
+        enqueue(0)
+        pool.sync()
+        alone = state[0]["out"].clone()
+        for _ in range(20):
+            enqueue(0)
+            enqueue(1)
+        pool.sync()
+        assert torch.equal(state[0]["out"], alone) and torch.equal(state[1]["out"], alone)
+    finally:
+        pool.destroy()
+
+
 def test_refusals_enqueue_nothing(pools):
     pool = pools()
     t = torch.zeros(4096, dtype=torch.float32, device="cuda")
