@@ -292,7 +292,7 @@ typedef struct {
     int residual_first;             /* 1: the residual is added before the activation */
     long long ldx, ldw, ldr, ldy;   /* between rows of x, w, residual, y; 0: k, k, n, n */
 } sgprs_linear_desc_t;
-/* Scratch needed on a partition of partition_cus CUs (0 where K is not split over workgroups). */
+/* Scratch needed on a partition of partition_cus CUs (0: none). */
 int sgprs_linear_workspace(const sgprs_linear_desc_t *d, int partition_cus, size_t *bytes);
 /* x [m][k], w [n][k], residual NULL or [m][n], y [m][n] DEVICE in dtype; bias
  * NULL or DEVICE fp32[n].  y may be the residual itself (same pointer and

@@ -228,7 +228,11 @@ __device__ __forceinline__ void tile_of(int id, int grid_m, int grid_n, int* tm,
 // BM x BN outputs, 2 x 2 wavefronts; two k-tiles in LDS, filled by loads that write it directly.  The barrier of a
 // k-tile stands between its two halves: before it the second half's fragments have been read, so that its MFMAs
 // follow the barrier at once while the next k-tile's first fragments are read and the one after that is requested
-// into the buffer just left.
+// into the buffer just left, a load behind every fourth MFMA (twice as fast: 447 us instead of 409 below).
+// Bound by the matrix cores at the clock they leave: 256 x 256 (one wavefront a SIMD, 256 accumulators; half the LDS
+// reads per MFMA of 128 x 128) keeps them 68 % busy at 1.9 GHz, 16384x4096 -> 4096 in 409 us, 1343 TFLOP/s, where a
+// large library product reaches 1529.  128 x 128 (two workgroups a CU) is for what 256 x 256 divides badly: a tile's
+// beginning and end cost as much as five k-tiles.
 template <int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM * BN >= 256 * 128 ? 1 : 2) void linear_tile_kernel(const LinearArgs a)
 {
 #if __HIP_DEVICE_COMPILE__
@@ -330,6 +334,11 @@ template <int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM * BN >= 
 // MFMAs for 32 inputs instead of eight that take twice as long.  A sum that is not finite (infinities have no such
 // parts, nor has what rounds up to one) or tiny (the parts of values below 2^-100 fall short of bf16's range) sends
 // its wavefront through the fp32 matrix cores.
+// 128 x 128, fp32: bound by the splitting (half of the vector units' time) and the MFMAs, 4096x4096 -> 4096 in 680 us,
+// 200 TFLOP/s; fp32 MFMAs on the same tiles reached 142, the rate of the fp32 matrix cores is 157.  Relative error
+// against 64 bits 1.6e-7 (plain fp32 chains 2.9e-7 to 7e-7).  64 x 64 with two groups of wavefronts that take every
+// other k-tile is for fewer tiles: the second group covers what the first one waits for (fp32 300x700 -> 700 19.9 -> 16.8,
+// 3136x512 -> 512 19.8 -> 17.4 us).
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ unsigned pack_bf16x2(float lo, float hi)
 {
@@ -563,6 +572,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void linear_staged_kernel(const Li
 // ---- few rows: K split over the wavefronts of a workgroup --------------------------------------
 // 16 TM x 16 TN outputs per workgroup; wavefront v takes k-tiles v, v + NW, ..., moves them into an LDS ring of
 // its own and meets the others at the end only, where the partial tiles are added in wavefront order.
+// Bound by reading w once and by the launch: 24x4096 -> 4096 bf16 in 8.5 us (4 TB/s), 1x512 -> 1000 in 3.8.
 template <int DT, int ACT, int TM, int TN, int NW, int NS, bool DIRECT>
 __global__ __launch_bounds__(NW * 64, 1) void linear_ksplit_kernel(const LinearArgs a)
 {
@@ -677,14 +687,17 @@ __global__ __launch_bounds__(NW * 64, 1) void linear_ksplit_kernel(const LinearA
 // ---- plans -------------------------------------------------------------------------------------
 enum LinearKernel { kTile256, kTile128, kStaged128, kStaged64, kSplit16, kSplit32x16, kSplit32 };
 
+// No kernel splits K over workgroups: with eight wavefronts sharing it, the few tiles where that could pay (K beyond 6000
+// at up to 64 rows and 512 outputs: 13 us) leave 4 us of it to gain behind a second launch.
 size_t linear_workspace_bytes(const sgprs_linear_desc_t&, int) { return 0; }
 
-// direct: operands whose rows are whole aligned chunks.  Estimates in us, from measurements on 256 CUs (inputs that
-// change, no residual): what a kernel's k-tile and its tile's beginning and end take, times the tiles of a CU.
-// bf16, 256 x 256 / 128 x 128 / staged 64 x 64: 16384x4096 -> 4096 427 / 508 / 800 us, 4096x4096 -> 4096 101 / 119 / 186,
-// 12544x512 -> 2048 46 / 42 / 52, 16384x512 -> 512 - / 15.1 / 20.9, 3136x512 -> 512 - / 9.3 / 7.0; K split over
-// wavefronts there 21, but 7.2 against 7.2 and 18 for 300x700 -> 700.  fp32, staged 128 x 128 / 64 x 64 / K split:
-// 4096x4096 -> 4096 677 / 836 / 1213, 16384x512 -> 512 55 / 70 / 140, 1000x1024 -> 1024 66 / 22 / 28, 300x700 -> 700 45 / 17 / 7.2.
+// direct: operands whose rows are whole aligned chunks.  Estimates in us, fitted to measurements on 256 CUs (three sets of
+// inputs in turn): what a kernel's k-tile and its tile's beginning and end take, times the tiles of a CU.
+// bf16, 256 x 256 / 128 x 128 / 64 x 64: 16384x4096 -> 4096 427 / 508 / 800 us, 4096x4096 -> 4096 101 / 119 / 186,
+// 12544x512 -> 2048 46 / 42 / 52, 16384x512 -> 512 - / 15.1 / 20.9, 3136x512 -> 512 - / 9.3 / 7.0 (K split over wavefronts
+// 21); 300x700 -> 700 18 / 7.2 / 7.6 for 128 x 128 / 64 x 64 / K split.  fp32, 128 x 128 / 64 x 64 / K split:
+// 4096x4096 -> 4096 677 / 894 / 1213, 16384x512 -> 512 55 / 71 / 140, 1000x1024 -> 1024 66 / 22 / 28, 300x700 -> 700
+// 45 / 17 / 7.2.
 static int plan_linear(const sgprs_linear_desc_t& d, int cus, bool direct)
 {
     auto tiles = [&](int b, int c) { return (double)((d.m + (long long)b - 1) / b) * ((d.n + c - 1) / c); };
