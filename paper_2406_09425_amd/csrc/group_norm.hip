@@ -191,12 +191,12 @@ template <int DT, bool WHOLE, int NV> struct NormShare {
     __device__ __forceinline__ NormShare(const NormArgs& a)
     {
         const int tid = threadIdx.x;
-        c0 = blockIdx.x * a.slice;
+        c0 = blockIdx.y * a.slice;
         channels = min(a.slice, a.c - c0);
         groups = a.slice_groups;
         if (channels < a.slice) groups = channels / a.per;
         image = blockIdx.z;
-        first = blockIdx.y * a.step * NV;
+        first = blockIdx.x * a.step * NV;
         rows = min(a.step * NV, a.hw - first);
         s = div_magic(tid, a.vec_mul, a.vec_sh);
         v = tid - s * a.vectors;
@@ -257,7 +257,7 @@ template <int DT, int ACT, bool WHOLE, int NV, bool FUSED> __global__ __launch_b
             const float t = N::get(x[k], e) - mean[e];
             sq[e] = __builtin_fmaf((WHOLE || e < m.live) && m.has(a, k) ? t : 0.f, t, sq[e]);
         }
-    float2* partial = a.partial + ((long long)m.image * a.chunks + blockIdx.y) * a.groups + blockIdx.x * a.slice_groups;
+    float2* partial = a.partial + ((long long)m.image * a.chunks + blockIdx.x) * a.groups + blockIdx.y * a.slice_groups;
     if constexpr (!FUSED) {
         for (int g = tid; g < m.groups; g += T) partial[g].x = total[g] * inv_count;
     }
@@ -298,7 +298,7 @@ template <int DT, int ACT, bool WHOLE, int NV> __global__ __launch_bounds__(1024
     N::per_channel(a.gamma ? a.gamma + c : nullptr, m.live, 1.f, gamma);
     N::per_channel(a.beta ? a.beta + c : nullptr, m.live, 0.f, beta);
     // Chunks of a group: `share` neighbouring lanes, in order.  All chunks but the last count `full` positions.
-    const float2* partial = a.partial + (long long)m.image * a.chunks * a.groups + blockIdx.x * a.slice_groups;
+    const float2* partial = a.partial + (long long)m.image * a.chunks * a.groups + blockIdx.y * a.slice_groups;
     float *means = lds, *scales = means + groups;
     const float inv_hw = 1.f / (float)a.hw;
     const int last = a.hw - (a.chunks - 1) * full;
@@ -479,7 +479,7 @@ template <int DT, int ACT, bool WHOLE> static int launch_norm(const NormArgs& a,
         default: SGPRS_LAUNCH((row_norm_kernel<DT, ACT, WHOLE, 8>), grid, 256, 0, stream, a);
         }
     } else {
-        const dim3 grid(p.slices, p.chunks, a.n);
+        const dim3 grid(p.chunks, p.slices, a.n);
         const size_t lds = sizeof(float) * ((size_t)p.threads * V + 2 * a.slice_groups);
         if (p.fused) {
             switch (p.nv) {
@@ -511,7 +511,8 @@ int launch_group_norm(const sgprs_group_norm_desc_t& d, const void* x, const flo
                       void* ws, hipStream_t stream, int cus)
 {
     const NormPlan p = plan_norm(d, cus);
-    if (!p.rows && (d.n > 65535 || p.chunks > 65535)) return fail(SGPRS_ERR_UNSUPPORTED, "%d images of %d positions", d.n, d.hw);
+    if (!p.rows && (d.n > 65535 || p.slices > 65535 || (long long)p.chunks * p.threads >= (1ll << 32)))
+        return fail(SGPRS_ERR_UNSUPPORTED, "%d images of %d positions and %d channels", d.n, d.hw, d.c);
     const long long es = (long long)dtype_size(d.dtype);
     const int V = 16 / (int)es;
     NormArgs a = {(const unsigned char*)x, gamma, beta, (const unsigned char*)residual, (unsigned char*)y, (float2*)ws, d.n, d.hw, d.c, d.groups,

@@ -715,7 +715,7 @@ static int plan_linear(const sgprs_linear_desc_t& d, int cus, bool direct)
 
 template <auto kernel> static int launch_sized(int lds, const LinearArgs& a, int threads, hipStream_t stream)
 {
-    if ((long long)a.grid_m * a.grid_n >= (1ll << 31)) return fail(SGPRS_ERR_UNSUPPORTED, "%d x %d outputs", a.m, a.n);
+    if ((long long)a.grid_m * a.grid_n * threads >= (1ll << 32)) return fail(SGPRS_ERR_UNSUPPORTED, "%d x %d outputs", a.m, a.n);
     static std::atomic<bool> raised{false};  // more than the default 64 KiB of dynamic LDS needs an opt-in per kernel
     if (lds > 65536 && !raised) {
         SGPRS_HIP(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));

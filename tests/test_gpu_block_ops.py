@@ -236,6 +236,26 @@ def run_norm(pools, name, n, hw, c, groups, act=0, affine=True, res=False, pads=
         assert torch.equal(call().nan_to_num(), got.nan_to_num()), f"{what}: a second call gives other bits"
 
 
+def test_group_norm_of_many_positions(pools):
+    """More chunks of positions than a grid's second dimension holds."""
+    hw, c = 600000, 2048
+    x = torch.empty(hw, c, dtype=torch.bfloat16, device="cuda").normal_()
+    y = torch.zeros_like(x)
+    d = S.GroupNormDesc(n=1, hw=hw, c=c, groups=8, dtype=S.SGPRS_BF16, eps=1e-5)
+    ws_bytes = S.sgprs_group_norm_workspace(d, CUS)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    pool = pools()
+    S.sgprs_group_norm(d, ptr(x), None, None, None, ptr(y), ptr(ws), ws_bytes, pool, 0)
+    pool.sync()
+    for at in (0, hw // 2, hw - 64):
+        part = x[at:at + 64].double().reshape(64, 8, 256)
+        mean = torch.stack([x[:, i * 256:(i + 1) * 256].float().mean().double() for i in range(8)])[None, :, None]
+        var = torch.stack([x[:, i * 256:(i + 1) * 256].float().var().double() for i in range(8)])[None, :, None]
+        want = ((part - mean) / (var + 1e-5).sqrt()).reshape(64, c)
+        assert float((y[at:at + 64].double() - want).abs().max()) <= 2.0 ** -8 * float(want.abs().max()) + 1e-4
+
+
 NORM = [(1, 1, 1, 1), (1, 1, 64, 1), (3, 1, 512, 1), (1000, 1, 512, 1), (77, 1, 1000, 1), (5, 1, 4096, 1), (9, 1, 33, 3), (1, 49, 512, 32), (2, 49, 512, 512),
         (13, 196, 256, 32), (4, 196, 256, 1), (2, 784, 128, 32), (1, 3136, 64, 32), (3, 3136, 64, 8), (1, 12544, 64, 32), (2, 5000, 320, 32), (3, 527, 96, 8),
         (2, 527, 99, 9), (1, 1, 2048, 32), (40, 7, 24, 24), (1, 20000, 8, 1), (2, 333, 1030, 1), (300, 2, 16, 4), (1, 9000, 512, 4)]
@@ -496,6 +516,26 @@ def test_attention_cache_beyond_32_bit_offsets(pools):
     pool.sync()
     want, bound = ref.attention(qh, kh[-m:], vh[-m:], [m], [m], True, 0.0)
     ref.assert_within(o.cpu(), want, bound, "the last tokens of a large buffer")
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("q_lens,kv_lens,max_q,max_kv", [([3, 1], [300, 500], 3, 40), ([200, 40], [900, 70], 200, 70), ([3, 60], [300, 500], 3, 500)], ids=str)
+def test_attention_sequences_longer_than_said(pools, name, q_lens, kv_lens, max_q, max_kv):
+    """Results are unspecified then; what lies beside the output stays as it is."""
+    dt, tdt = DT[name]
+    heads, dim, tq, tk = 2, 64, sum(q_lens), sum(kv_lens)
+    g = gen(2)
+    q, k, v = (torch.randn(t, heads * dim, generator=g).to(tdt).cuda() for t in (tq, tk, tk))
+    out = torch.full((tq + 8, heads * dim), 777.0, dtype=tdt, device="cuda")
+    d = S.AttentionDesc(n_seqs=2, total_q=tq, total_kv=tk, max_q=max_q, max_kv=max_kv, heads=heads, kv_heads=heads, head_dim=dim, dtype=dt, causal=1)
+    ws_bytes = S.sgprs_attention_workspace(d, CUS)
+    ws = torch.full((ws_bytes + 4096,), 9, dtype=torch.uint8, device="cuda")
+    qo, ko = offsets(q_lens), offsets(kv_lens)
+    torch.cuda.synchronize()
+    pool = pools()
+    S.sgprs_attention(d, ptr(q), ptr(k), ptr(v), ptr(qo), ptr(ko), ptr(out), ptr(ws) if ws_bytes else None, ws_bytes, pool, 0)
+    pool.sync()
+    assert bool((out[tq:] == 777.0).all()) and bool((ws[ws_bytes:] == 9).all())
 
 
 # ---- all together --------------------------------------------------------------------------------
