@@ -392,7 +392,8 @@ def test_attention_grouped_heads(pools, name, heads, kv_heads, q_lens, kv_lens):
 @pytest.mark.parametrize("name", ["f32", "bf16"])
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("q_lens,kv_lens", [([1], [1]), ([1], [5000]), ([1, 1, 1, 1], [1025, 0, 64, 2049]), ([2, 1, 3], [700, 63, 129]), ([5, 0, 7], [4097, 12, 7]),
-                                            ([1] * 20, list(range(50, 1050, 50))), ([16], [3000]), ([17], [1500])], ids=str)
+                                            ([1] * 20, list(range(50, 1050, 50))), ([16], [3000]), ([17], [1500]),
+                                            ([50, 7], [1700, 90]), ([61], [1000])], ids=str)
 @pytest.mark.parametrize("heads,kv_heads,dim", [(8, 2, 128), (3, 3, 64)])
 def test_attention_against_caches(pools, name, causal, q_lens, kv_lens, heads, kv_heads, dim):
     run_attention(pools, name, q_lens, kv_lens, heads, kv_heads, dim, causal, seed=len(q_lens))
