@@ -331,9 +331,12 @@ template <int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM * BN >= 
 // multiplied.  A thread brings units of 8 neighbouring inputs of a row.  fp32 goes through the bf16 matrix cores:
 // x = h + m + l, each the bf16 nearest to what is left, holds 24 bits, and of the nine products of two such sums the
 // six down to 2^-16 are taken (what is left out stays below 2^-23 of a product, and is of either sign); that is six
-// MFMAs for 32 inputs instead of eight that take twice as long.  A sum that is not finite (infinities have no such
-// parts, nor has what rounds up to one) or tiny (the parts of values below 2^-100 fall short of bf16's range) sends
-// its wavefront through the fp32 matrix cores.
+// MFMAs for 32 inputs instead of eight that take twice as long.  Both operands are multiplied by 2^24 first: so the parts
+// of small and subnormal values hold all their bits too, the first one as a normal number (the matrix cores align a
+// subnormal operand's products as if they had its leading zeros in front: with 2^16, which takes 2^-149 to bf16's smallest
+// number, 2^-149 times ordinary values was off by 2^-17).  A sum that is not finite then (infinities have no such parts;
+// operands from 2^104 and sums from 2^80 on pass the range) sends its wavefront through the fp32 matrix cores, with the
+// operands as they are.
 // 128 x 128, fp32: bound by the splitting (half of the vector units' time) and the MFMAs, 4096x4096 -> 4096 in 680 us,
 // 200 TFLOP/s; fp32 MFMAs on the same tiles reached 142, the rate of the fp32 matrix cores is 157.  Relative error
 // against 64 bits 1.6e-7 (plain fp32 chains 2.9e-7 to 7e-7).  64 x 64 with two groups of wavefronts that take every
@@ -345,6 +348,7 @@ __device__ __forceinline__ unsigned pack_bf16x2(float lo, float hi)
     const f32x2_t f = {lo, hi};
     return __builtin_bit_cast(unsigned, __builtin_convertvector(f, bf16x2_t));
 }
+constexpr float kSplitScale = 0x1p24f;
 template <int DT> __device__ __forceinline__ void split_unit(const u32x4_t* in, u32x4_t* planes)
 {
     if constexpr (DT == SGPRS_BF16) {
@@ -352,7 +356,7 @@ template <int DT> __device__ __forceinline__ void split_unit(const u32x4_t* in, 
     } else {
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            float a = __uint_as_float(in[p >> 1][2 * (p & 1)]), b = __uint_as_float(in[p >> 1][2 * (p & 1) + 1]);
+            float a = __uint_as_float(in[p >> 1][2 * (p & 1)]) * kSplitScale, b = __uint_as_float(in[p >> 1][2 * (p & 1) + 1]) * kSplitScale;
 #pragma unroll
             for (int i = 0; i < 3; ++i) {
                 const unsigned v = pack_bf16x2(a, b);
@@ -538,8 +542,8 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void linear_staged_kernel(const Li
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float size = fabsf(acc[j][i][e]);
-                    again |= !(size < 3e38f) || (size < 1e-18f && size > 0.f);
+                    again |= !(fabsf(acc[j][i][e]) < INFINITY);
+                    acc[j][i][e] *= 1.f / (kSplitScale * kSplitScale);
                 }
         if (__any(again)) {
 #pragma unroll

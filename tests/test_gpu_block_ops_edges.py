@@ -1,0 +1,45 @@
+"""GPU parity of the attention-block operators with 64-bit definitions at the edges of what their descriptors allow:
+operands at the ends of fp32's range, more rows, images and sequences than a launch or a search step takes at once."""
+import math
+
+import pytest
+import torch
+
+import paper_2406_09425_amd as S
+import block_ops_util as ref
+from test_gpu_block_ops import CUS, DT, gen, offsets, pools, ptr, run_attention, run_norm  # noqa: F401 (pools is a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- linear --------------------------------------------------------------------------------------
+def linear_plain(pools, xh, wh, cus=CUS, act=0):
+    """x w^T of dense tensors, no bias, no residual."""
+    (m, k), n = xh.shape, wh.shape[0]
+    x, w = xh.cuda(), wh.cuda()
+    y = torch.full((m, n), float("nan"), dtype=xh.dtype, device="cuda")
+    d = S.LinearDesc(m=m, n=n, k=k, dtype=S.SGPRS_F32 if xh.dtype == torch.float32 else S.SGPRS_BF16, act=act)
+    ws_bytes = S.sgprs_linear_workspace(d, cus)
+    ws = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    pool = pools(cus)
+    S.sgprs_linear(d, ptr(x), ptr(w), None, None, ptr(y), ptr(ws), ws_bytes, pool, 0)
+    pool.sync()
+    return y.cpu()
+
+
+@pytest.mark.parametrize("small,large", [(116, 112), (122, 118), (126, 122), (135, 123), (140, 100), (138, 0), (66, -72)])
+@pytest.mark.parametrize("m,n,k,cus", [(20, 140, 96, 256), (2100, 700, 96, 256), (2050, 570, 101, 256), (600, 700, 40, 8)])
+@pytest.mark.parametrize("swap", [False, True])
+def test_linear_fp32_operands_near_the_ends_of_the_range(pools, small, large, m, n, k, cus, swap):
+    """Small and subnormal values against ordinary and large ones: every operand counts with its 24 bits.  Beside the
+    usual bound, each product (in up to six parts) and each addition may round by half of fp32's smallest number."""
+    g = gen(small)
+    x, w = torch.randn(m, k, generator=g), torch.randn(n, k, generator=g)
+    (w if swap else x).mul_(2.0 ** -small)
+    (x if swap else w).mul_(2.0 ** large)
+    x[5] = 0.0
+    x[6] = 0.0
+    x[6, 3] = 2.0 ** -149
+    want, bound = ref.linear(x, w, None, None, 0, 0)
+    ref.assert_within(linear_plain(pools, x, w, cus), want, bound + 8 * k * 2.0 ** -149, f"2^-{small} against 2^{large}, {m}x{k}->{n}")
