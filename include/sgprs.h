@@ -331,7 +331,9 @@ int sgprs_group_norm(const sgprs_group_norm_desc_t *d, const void *x, const floa
  * so query i of nq sees keys j <= i + nk - nq.  A query that sees no key gets
  * zeros; what k and v hold at keys that a query does not see (NaN included)
  * does not reach it.  One query per sequence against a cache is the case of
- * max_q = 1. */
+ * max_q = 1.  UNSUPPORTED: calls that would take 2^24 workgroups (of 128 queries
+ * of a head; where max_q is small, of 32 queries times heads of a key head, and of
+ * one query of a head where a cache is split). */
 typedef struct {
     int n_seqs;
     int total_q, total_kv;          /* tokens in q and o, in k and v */

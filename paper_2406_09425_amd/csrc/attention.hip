@@ -771,9 +771,14 @@ size_t attention_workspace_bytes(const sgprs_attention_desc_t& d, int cus)
     return p.chunks > 1 ? (size_t)p.chunks * d.total_q * d.heads * (d.head_dim * sizeof(float) + sizeof(float2)) : 0;
 }
 
+constexpr long long kMaxGrid = (1ll << 24) - 1;  // workgroups of 256 threads: a launch has less than 2^32 threads
+static int too_large(const AttentionArgs& a)
+{
+    return fail(SGPRS_ERR_UNSUPPORTED, "%d sequences of %d tokens and %d heads", a.n_seqs, a.total_q, a.heads);
+}
+
 template <auto kernel> static int launch_sized(long long grid, int threads, int lds, const AttentionArgs& a, hipStream_t stream)
 {
-    if (grid * threads >= (1ll << 32)) return fail(SGPRS_ERR_UNSUPPORTED, "%d sequences of %d tokens and %d heads", a.n_seqs, a.total_q, a.heads);
     static std::atomic<bool> raised{false};  // more than the default 64 KiB of dynamic LDS needs an opt-in per kernel
     if (lds > 65536 && !raised) {
         SGPRS_HIP(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
@@ -789,15 +794,19 @@ template <int DT, int HD> static int launch_shape(AttentionArgs a, bool decode, 
     if (!decode) {
         a.slots = a.total_q / kPromptRows + a.n_seqs;
         a.tile_rows = kPromptRows;
-        if ((long long)a.slots * a.heads >= (1ll << 31)) return fail(SGPRS_ERR_UNSUPPORTED, "%d sequences of %d tokens and %d heads", a.n_seqs, a.total_q, a.heads);
-        const int rc = launch_sized<attention_prompt_kernel<DT, HD>>((long long)a.chunks * a.slots * a.heads, 256, PromptShape<DT, HD>::STAGES * PromptShape<DT, HD>::STAGE, a, stream);
+        const long long grid = (long long)a.chunks * a.slots * a.heads, join = ((long long)a.total_q * a.heads + 3) / 4;
+        if (grid > kMaxGrid || (a.chunks > 1 && join > kMaxGrid)) return too_large(a);  // (before anything is enqueued)
+        const int rc = launch_sized<attention_prompt_kernel<DT, HD>>(grid, 256, PromptShape<DT, HD>::STAGES * PromptShape<DT, HD>::STAGE, a, stream);
         if (rc || a.chunks == 1) return rc;
-        return launch_sized<attention_join_kernel<DT, 4>>(((long long)a.total_q * a.heads + 3) / 4, 256, 0, a, stream);
+        return launch_sized<attention_join_kernel<DT, 4>>(join, 256, 0, a, stream);
     }
     typedef DecodeShape<DT, HD> Shape;
-    const int rc = launch_sized<attention_decode_kernel<DT, HD>>((long long)a.chunks * a.n_seqs * a.row_blocks * a.kv_heads, Shape::NW * 64, Shape::LDS, a, stream);
+    static_assert(Shape::NW * 64 == 256, "kMaxGrid's workgroups");
+    const long long grid = (long long)a.chunks * a.n_seqs * a.row_blocks * a.kv_heads, join = (long long)a.total_q * a.heads;
+    if (grid > kMaxGrid || (a.chunks > 1 && join > kMaxGrid)) return too_large(a);
+    const int rc = launch_sized<attention_decode_kernel<DT, HD>>(grid, Shape::NW * 64, Shape::LDS, a, stream);
     if (rc || a.chunks == 1) return rc;
-    return launch_sized<attention_join_kernel<DT, 1>>((long long)a.total_q * a.heads, 256, 0, a, stream);
+    return launch_sized<attention_join_kernel<DT, 1>>(join, 256, 0, a, stream);
 }
 
 template <int DT> static int launch_typed(const AttentionArgs& a, bool decode, hipStream_t stream)

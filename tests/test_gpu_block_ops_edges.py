@@ -43,3 +43,26 @@ def test_linear_fp32_operands_near_the_ends_of_the_range(pools, small, large, m,
     x[6, 3] = 2.0 ** -149
     want, bound = ref.linear(x, w, None, None, 0, 0)
     ref.assert_within(linear_plain(pools, x, w, cus), want, bound + 8 * k * 2.0 ** -149, f"2^-{small} against 2^{large}, {m}x{k}->{n}")
+
+
+# ---- attention -----------------------------------------------------------------------------------
+def test_attention_of_more_pairs_than_a_join_takes_enqueues_nothing(pools):
+    """2^24 (token, head) pairs whose keys are split: the second launch is too large, so the first must not run."""
+    n, heads, dim, keys = 1 << 19, 32, 8, 256
+    q = torch.zeros(n, heads * dim, dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros(keys, dim, dtype=torch.bfloat16, device="cuda")
+    o = torch.full_like(q, 777.0)
+    q_offsets = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    kv_offsets = torch.full((n + 1,), keys, dtype=torch.int32, device="cuda")
+    kv_offsets[0] = 0
+    d = S.AttentionDesc(n_seqs=n, total_q=n, total_kv=keys, max_q=1, max_kv=keys, heads=heads, kv_heads=1, head_dim=dim, dtype=S.SGPRS_BF16)
+    ws_bytes = S.sgprs_attention_workspace(d, CUS)
+    assert ws_bytes > 0  # keys are split
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    pool = pools()
+    with pytest.raises(S.SgprsError) as e:
+        S.sgprs_attention(d, ptr(q), ptr(k), ptr(k), ptr(q_offsets), ptr(kv_offsets), ptr(o), ptr(ws), ws_bytes, pool, 0)
+    assert e.value.status == -5
+    pool.sync()
+    assert bool((o == 777.0).all())
