@@ -307,7 +307,7 @@ int sgprs_linear(const sgprs_linear_desc_t *d, const void *x, const void *w, con
  * all hw positions, and
  *   y = act( (x - mean) / sqrt(var + eps) * gamma[c] + beta[c] (+ residual) ).
  * With hw = 1 and groups = 1 it is the layer norm of n tokens.  UNSUPPORTED: groups of more
- * than 16 KiB of channels, more than 65535 images (layer norms aside). */
+ * than 16 KiB of channels. */
 typedef struct {
     int n, hw, c, groups;           /* c % groups == 0 */
     int dtype;                      /* of x, residual, y */

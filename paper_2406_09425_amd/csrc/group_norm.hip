@@ -507,11 +507,14 @@ template <int DT, bool WHOLE> static int launch_norm_act(const NormArgs& a, cons
     }
 }
 
+// Images that a launch takes: its grid's third dimension.
+constexpr int kMaxImages = 65535;
+
 int launch_group_norm(const sgprs_group_norm_desc_t& d, const void* x, const float* gamma, const float* beta, const void* residual, void* y,
                       void* ws, hipStream_t stream, int cus)
 {
     const NormPlan p = plan_norm(d, cus);
-    if (!p.rows && (d.n > 65535 || p.slices > 65535 || (long long)p.chunks * p.threads >= (1ll << 32)))
+    if (!p.rows && (p.slices > 65535 || (long long)p.chunks * p.threads >= (1ll << 32)))
         return fail(SGPRS_ERR_UNSUPPORTED, "%d images of %d positions and %d channels", d.n, d.hw, d.c);
     const long long es = (long long)dtype_size(d.dtype);
     const int V = 16 / (int)es;
@@ -524,9 +527,24 @@ int launch_group_norm(const sgprs_group_norm_desc_t& d, const void* x, const flo
         while (a.share_log2 < 6 && (2 << a.share_log2) * a.slice_groups <= p.threads) ++a.share_log2;
     }
     const bool whole = d.c % V == 0 && (p.rows || p.slice % V == 0);
-    if (d.dtype == SGPRS_BF16)
-        return whole ? launch_norm_act<SGPRS_BF16, true>(a, p, d.act, cus, stream) : launch_norm_act<SGPRS_BF16, false>(a, p, d.act, cus, stream);
-    return whole ? launch_norm_act<SGPRS_F32, true>(a, p, d.act, cus, stream) : launch_norm_act<SGPRS_F32, false>(a, p, d.act, cus, stream);
+    for (long long first = 0; first < d.n; first += kMaxImages) {
+        NormArgs part = a;
+        if (!p.rows) {
+            const long long positions = first * d.hw;
+            part.n = (int)std::min<long long>(kMaxImages, d.n - first);
+            part.x += positions * a.ldx;
+            if (a.residual) part.residual += positions * a.ldr;
+            part.y += positions * a.ldy;
+            part.partial += first * p.chunks * d.groups;
+        }
+        int rc;
+        if (d.dtype == SGPRS_BF16)
+            rc = whole ? launch_norm_act<SGPRS_BF16, true>(part, p, d.act, cus, stream) : launch_norm_act<SGPRS_BF16, false>(part, p, d.act, cus, stream);
+        else
+            rc = whole ? launch_norm_act<SGPRS_F32, true>(part, p, d.act, cus, stream) : launch_norm_act<SGPRS_F32, false>(part, p, d.act, cus, stream);
+        if (rc || p.rows) return rc;
+    }
+    return SGPRS_OK;
 }
 
 }  // namespace sgprs

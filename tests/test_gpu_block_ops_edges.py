@@ -66,3 +66,50 @@ def test_attention_of_more_pairs_than_a_join_takes_enqueues_nothing(pools):
     assert e.value.status == -5
     pool.sync()
     assert bool((o == 777.0).all())
+
+
+# ---- group norm ----------------------------------------------------------------------------------
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("extra", [8, 9])
+def test_layer_norms_of_wide_rows_and_many_tokens(pools, name, extra):
+    """Rows just beyond those that a wavefront holds, more of them than a launch has images."""
+    dt, tdt = DT[name]
+    n, c = 70000, (2048 if name == "f32" else 4096) + extra
+    x = torch.empty(n, c, dtype=tdt, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(extra))
+    y = torch.zeros_like(x)
+    gamma = torch.rand(c, generator=gen(1)) + 0.5
+    G = gamma.cuda()
+    d = S.GroupNormDesc(n=n, hw=1, c=c, groups=1, dtype=dt, eps=1e-5)
+    ws_bytes = S.sgprs_group_norm_workspace(d, CUS)
+    ws = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    pool = pools()
+    S.sgprs_group_norm(d, ptr(x), ptr(G), None, None, ptr(y), ptr(ws), ws_bytes, pool, 0)
+    pool.sync()
+    for at in (0, 65530, n - 8):
+        want, bound = ref.group_norm(x[at:at + 8].cpu(), gamma, None, None, 8, 1, 1, 1e-5, 0)
+        ref.assert_within(y[at:at + 8], want, bound, f"rows {at} and on of {n} of {c}")
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("hw,c,groups", [(1, 16, 4), (3, 9, 3)])
+def test_group_norms_of_more_images_than_a_launch_takes(pools, name, hw, c, groups):
+    run_norm(pools, name, 131075, hw, c, groups, act=3, res=True, seed=c)
+
+
+def test_group_norms_of_more_large_images_than_a_launch_takes(pools):
+    """Statistics of chunks in the workspace, for each of the launches."""
+    n, hw, c, groups = 65537, 257, 256, 1
+    d = S.GroupNormDesc(n=n, hw=hw, c=c, groups=groups, dtype=S.SGPRS_BF16, eps=1e-5)
+    ws_bytes = S.sgprs_group_norm_workspace(d, CUS)
+    assert ws_bytes > 0
+    x = torch.empty(n, hw, c, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(3))
+    y = torch.zeros_like(x)
+    ws = torch.full((max(ws_bytes, 16),), 255, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    pool = pools()
+    S.sgprs_group_norm(d, ptr(x), None, None, None, ptr(y), ptr(ws), ws_bytes, pool, 0)
+    pool.sync()
+    for at in (0, 65534, 65535, 65536):
+        want, bound = ref.group_norm(x[at].cpu(), None, None, None, 1, hw, groups, 1e-5, 0)
+        ref.assert_within(y[at], want, bound, f"image {at} of {n}")
