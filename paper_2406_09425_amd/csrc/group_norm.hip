@@ -457,7 +457,7 @@ static NormPlan plan_norm(const sgprs_group_norm_desc_t& d, int cus)
         p.nv = 8;
     }
     p.step = std::max(1, p.threads / p.vectors);
-    p.chunks = (d.hw + p.step * p.nv - 1) / (p.step * p.nv);
+    p.chunks = (d.hw - 1) / (p.step * p.nv) + 1;  // (hw may be the largest int)
     return p;
 }
 
@@ -471,7 +471,7 @@ template <int DT, int ACT, bool WHOLE> static int launch_norm(const NormArgs& a,
 {
     constexpr int V = NormVec<DT, WHOLE>::V;
     if (p.rows) {
-        const dim3 grid(std::min((a.n + 3) / 4, 8 * cus));
+        const dim3 grid(std::min((a.n - 1) / 4 + 1, 8 * cus));
         switch (p.rows) {
         case 1: SGPRS_LAUNCH((row_norm_kernel<DT, ACT, WHOLE, 1>), grid, 256, 0, stream, a); break;
         case 2: SGPRS_LAUNCH((row_norm_kernel<DT, ACT, WHOLE, 2>), grid, 256, 0, stream, a); break;

@@ -732,8 +732,8 @@ template <auto kernel> static int launch_sized(int lds, const LinearArgs& a, int
 
 static LinearArgs tiled(LinearArgs a, int bm, int bn)
 {
-    a.grid_m = (a.m + bm - 1) / bm;
-    a.grid_n = (a.n + bn - 1) / bn;
+    a.grid_m = (a.m - 1) / bm + 1;  // (m may be the largest int)
+    a.grid_n = (a.n - 1) / bn + 1;
     return a;
 }
 

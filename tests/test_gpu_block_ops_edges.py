@@ -45,6 +45,18 @@ def test_linear_fp32_operands_near_the_ends_of_the_range(pools, small, large, m,
     ref.assert_within(linear_plain(pools, x, w, cus), want, bound + 8 * k * 2.0 ** -149, f"2^-{small} against 2^{large}, {m}x{k}->{n}")
 
 
+def test_linear_of_the_largest_number_of_rows_is_refused(pools):
+    """More tiles than a launch takes, counted without wrapping; nothing of the tensors is touched."""
+    x = torch.zeros(64, dtype=torch.bfloat16, device="cuda")
+    y = torch.full((64,), 777.0, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    for m in (2 ** 31 - 1, 2 ** 31 - 20):
+        with pytest.raises(S.SgprsError) as e:
+            S.sgprs_linear(S.LinearDesc(m=m, n=1, k=1, dtype=S.SGPRS_BF16), ptr(x), ptr(x), None, None, ptr(y), None, 0, pools(), 0)
+        assert e.value.status == -5
+    assert bool((y == 777.0).all())
+
+
 # ---- attention -----------------------------------------------------------------------------------
 def test_attention_of_more_pairs_than_a_join_takes_enqueues_nothing(pools):
     """2^24 (token, head) pairs whose keys are split: the second launch is too large, so the first must not run."""
