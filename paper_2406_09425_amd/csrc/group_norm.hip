@@ -6,7 +6,8 @@
 // (sum, then squares of the deviations from the mean), so nothing cancels, whatever the mean:
 //   * one launch where an image's positions of a slice of whole groups fit one workgroup's registers;
 //   * else one launch for the statistics of chunks of positions (mean and sum of squares of each group, in the
-//     workspace) and one that merges an image's chunks and writes the results;
+//     workspace) and one that merges an image's chunks and writes the results; with many chunks, which every
+//     workgroup would have to read, a launch between the two merges them;
 //   * a norm over all channels of single positions (layer norm) is a wavefront per row.
 // 64 images of 112 x 112 x 64 bf16 with residual and SiLU: 88 us, 26 of them statistics (x once, 4 TB/s) and 62 results
 // (x from the caches, residual, y: 4.9 TB/s, what a copy reaches).  12544 layer norms of 512 bf16 channels 6.6 us
@@ -26,6 +27,7 @@ struct NormArgs {
     const unsigned char* residual;
     unsigned char* y;
     float2* partial;         // [image][chunk][group]: mean, sum of the squared deviations
+    float2* merged;          // [image][group]: mean, 1 / deviation; NULL: each workgroup merges the chunks itself
     int n, hw, c, groups, per;
     unsigned per_mul;
     int per_sh;              // channel / per
@@ -281,7 +283,35 @@ template <int DT, int ACT, bool WHOLE, int NV, bool FUSED> __global__ __launch_b
     }
 }
 
-// Merges an image's chunks and writes the results of one of them.
+// Merges the chunks of a group of an image, over the lanes of a workgroup in a fixed order; all but the last chunk
+// count `full` positions.
+__global__ __launch_bounds__(256) void group_norm_merge_kernel(const NormArgs a, int full)
+{
+    __shared__ float sums[8];
+    const int tid = threadIdx.x, group = blockIdx.x, image = blockIdx.y, last = a.hw - (a.chunks - 1) * full;
+    const float2* from = a.partial + (long long)image * a.chunks * a.groups + group;
+    const float inv_hw = 1.f / (float)a.hw;
+    auto count = [&](int k) { return (float)(k == a.chunks - 1 ? last : full); };
+    auto all = [&](float v, float* s) {
+        v = lanes_sum(v, 64);
+        if ((tid & 63) == 0) s[tid >> 6] = v;
+        __syncthreads();
+        return (s[0] + s[1]) + (s[2] + s[3]);
+    };
+    float mean = 0.f, m2 = 0.f;
+#pragma unroll 4
+    for (int k = tid; k < a.chunks; k += 256) mean += from[(long long)k * a.groups].x * count(k);
+    mean = all(mean, sums) * inv_hw;
+#pragma unroll 4
+    for (int k = tid; k < a.chunks; k += 256) {
+        const float2 one = from[(long long)k * a.groups];
+        m2 += one.y + (one.x - mean) * (one.x - mean) * (count(k) * (float)a.per);
+    }
+    m2 = all(m2, sums + 4);
+    if (tid == 0) a.merged[(long long)image * a.groups + group] = make_float2(mean, __builtin_amdgcn_rsqf(m2 * inv_hw / (float)a.per + a.eps));
+}
+
+// Merges an image's chunks, if that is not done, and writes the results of one of them.
 template <int DT, int ACT, bool WHOLE, int NV> __global__ __launch_bounds__(1024) void group_norm_apply_kernel(const NormArgs a)
 {
     typedef NormVec<DT, WHOLE> N;
@@ -303,7 +333,14 @@ template <int DT, int ACT, bool WHOLE, int NV> __global__ __launch_bounds__(1024
     const float inv_hw = 1.f / (float)a.hw;
     const int last = a.hw - (a.chunks - 1) * full;
     const int share = 1 << a.share_log2, part = tid & (share - 1);
-    for (int g0 = 0; g0 < groups; g0 += T >> a.share_log2) {
+    if (a.merged) {
+        const float2* merged = a.merged + (long long)m.image * a.groups + blockIdx.y * a.slice_groups;
+        for (int g = tid; g < groups; g += T) {
+            means[g] = merged[g].x;
+            scales[g] = merged[g].y;
+        }
+    }
+    for (int g0 = a.merged ? groups : 0; g0 < groups; g0 += T >> a.share_log2) {
         const int g = g0 + (tid >> a.share_log2);
         const float2* from = partial + min(g, groups - 1);
         float mean = 0.f, m2 = 0.f;
@@ -408,7 +445,7 @@ template <int DT, int ACT, bool WHOLE, int NV> __global__ __launch_bounds__(256)
 // ---- plans -------------------------------------------------------------------------------------
 struct NormPlan {
     int rows;      // vectors a lane of the row kernel, 0: another kernel
-    bool fused;
+    bool fused, merge;
     int threads, nv, slice, vectors, step, chunks, slices;
 };
 
@@ -458,13 +495,18 @@ static NormPlan plan_norm(const sgprs_group_norm_desc_t& d, int cus)
     }
     p.step = std::max(1, p.threads / p.vectors);
     p.chunks = (d.hw - 1) / (p.step * p.nv) + 1;  // (hw may be the largest int)
+    // Workgroups that merge the chunks themselves read n slices chunks^2 groups pairs from the caches, twice; a launch of its
+    // own for that costs 3 us.  Worth it from 40 KB a CU on; without it / with it, 256 CUs, 32 groups: one image of 12544
+    // positions, 64 channels bf16 (1 MB) 10.4 / 11.7 us, 8 of them (10 MB) 15.1 / 15.1, 64 (79 MB) 90.7 / 78.6; one of 3136,
+    // 512 channels fp32 (20 MB) 12.8 / 11.5, of 12544 (315 MB) 77 / 18.7.
+    p.merge = !p.fused && 16.0 * d.n * p.slices * p.chunks * p.chunks * (p.slice / per) > 40e3 * cus;
     return p;
 }
 
 size_t group_norm_workspace_bytes(const sgprs_group_norm_desc_t& d, int cus)
 {
     const NormPlan p = plan_norm(d, cus);
-    return p.rows || p.fused ? 0 : (size_t)d.n * p.chunks * d.groups * sizeof(float2);
+    return p.rows || p.fused ? 0 : (size_t)d.n * (p.chunks + (p.merge ? 1 : 0)) * d.groups * sizeof(float2);
 }
 
 template <int DT, int ACT, bool WHOLE> static int launch_norm(const NormArgs& a, const NormPlan& p, int cus, hipStream_t stream)
@@ -490,6 +532,7 @@ template <int DT, int ACT, bool WHOLE> static int launch_norm(const NormArgs& a,
             }
         } else {
             SGPRS_LAUNCH((group_norm_chunk_kernel<DT, SGPRS_ACT_NONE, WHOLE, 8, false>), grid, p.threads, lds, stream, a);
+            if (p.merge) SGPRS_LAUNCH(group_norm_merge_kernel, dim3(a.groups, a.n), 256, 0, stream, a, p.step * p.nv);
             SGPRS_LAUNCH((group_norm_apply_kernel<DT, ACT, WHOLE, 8>), grid, p.threads, lds, stream, a);
         }
     }
@@ -518,7 +561,8 @@ int launch_group_norm(const sgprs_group_norm_desc_t& d, const void* x, const flo
         return fail(SGPRS_ERR_UNSUPPORTED, "%d images of %d positions and %d channels", d.n, d.hw, d.c);
     const long long es = (long long)dtype_size(d.dtype);
     const int V = 16 / (int)es;
-    NormArgs a = {(const unsigned char*)x, gamma, beta, (const unsigned char*)residual, (unsigned char*)y, (float2*)ws, d.n, d.hw, d.c, d.groups,
+    NormArgs a = {(const unsigned char*)x, gamma, beta, (const unsigned char*)residual, (unsigned char*)y, (float2*)ws,
+                  p.merge ? (float2*)ws + (size_t)d.n * p.chunks * d.groups : nullptr, d.n, d.hw, d.c, d.groups,
                   d.c / d.groups, 0, 0, d.ldx * es, d.ldr * es, d.ldy * es, d.eps, p.slice, p.vectors, p.step, 0, 0, 0, 0, p.chunks};
     div_constants(a.per, &a.per_mul, &a.per_sh);
     if (!p.rows) {
@@ -536,6 +580,7 @@ int launch_group_norm(const sgprs_group_norm_desc_t& d, const void* x, const flo
             if (a.residual) part.residual += positions * a.ldr;
             part.y += positions * a.ldy;
             part.partial += first * p.chunks * d.groups;
+            if (p.merge) part.merged += first * d.groups;
         }
         int rc;
         if (d.dtype == SGPRS_BF16)

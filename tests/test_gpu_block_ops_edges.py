@@ -1,6 +1,6 @@
 """GPU parity of the attention-block operators with 64-bit definitions at the edges of what their descriptors allow:
 operands at the ends of fp32's range, more rows, images and sequences than a launch or a search step takes at once."""
-import math
+import time
 
 import pytest
 import torch
@@ -55,6 +55,68 @@ def test_linear_of_the_largest_number_of_rows_is_refused(pools):
             S.sgprs_linear(S.LinearDesc(m=m, n=1, k=1, dtype=S.SGPRS_BF16), ptr(x), ptr(x), None, None, ptr(y), None, 0, pools(), 0)
         assert e.value.status == -5
     assert bool((y == 777.0).all())
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("shape,cus", [((1, 12544, 256, 32), 256), ((2, 6000, 96, 3), 40), ((1, 3000, 1030, 5), 8), ((3, 4100, 64, 64), 128), ((1, 700, 4096, 4096), 256)], ids=str)
+@pytest.mark.parametrize("inplace", [None, "x", "residual"])
+def test_group_norms_of_many_chunks(pools, name, shape, cus, inplace):
+    """Chunks that a launch of its own merges; odd numbers of groups and channels, slices of a row."""
+    run_norm(pools, name, *shape, act=3, res=True, cus=cus, seed=4, inplace=inplace)
+
+
+def test_group_norm_of_many_chunks_with_a_mean_far_from_zero(pools):
+    n, hw, c, groups = 1, 20000, 96, 4
+    run_norm(pools, "f32", n, hw, c, groups, x=torch.randn(n * hw, c, generator=gen(1)) + 1000.0, seed=1)
+
+
+def test_group_norm_takes_time_by_its_positions(pools):
+    """600000 positions are 75000 chunks: as long as a few copies of the tensor, not as chunks that each merge all others."""
+    hw, c = 600000, 2048
+    x = torch.empty(hw, c, dtype=torch.bfloat16, device="cuda").normal_()
+    y = torch.zeros_like(x)
+    d = S.GroupNormDesc(n=1, hw=hw, c=c, groups=8, dtype=S.SGPRS_BF16, eps=1e-5)
+    ws_bytes = S.sgprs_group_norm_workspace(d, CUS)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    pool = pools()
+
+    def seconds(call):
+        call()
+        pool.sync()
+        torch.cuda.synchronize()
+        begin = time.perf_counter()
+        call()
+        pool.sync()
+        torch.cuda.synchronize()
+        return time.perf_counter() - begin
+
+    copy = seconds(lambda: y.copy_(x))
+    norm = seconds(lambda: S.sgprs_group_norm(d, ptr(x), None, None, None, ptr(y), ptr(ws), ws_bytes, pool, 0))
+    assert norm <= 25 * copy, (norm, copy)
+
+
+def test_group_norm_of_the_largest_number_of_positions(pools):
+    hw = 2 ** 31 - 1
+    x = torch.empty(hw, 1, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(5))
+    x += 1.0
+    y = torch.zeros_like(x)
+    d = S.GroupNormDesc(n=1, hw=hw, c=1, groups=1, dtype=S.SGPRS_BF16, eps=1e-5)
+    ws_bytes = S.sgprs_group_norm_workspace(d, CUS)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    pool = pools()
+    S.sgprs_group_norm(d, ptr(x), None, None, None, ptr(y), ptr(ws), ws_bytes, pool, 0)
+    pool.sync()
+    sums = torch.zeros(2, dtype=torch.float64)
+    for at in range(0, hw, 1 << 27):
+        part = x[at:at + (1 << 27)].double()
+        sums += torch.stack([part.sum(), (part * part).sum()]).cpu()
+    mean = sums[0] / hw
+    deviation = (sums[1] / hw - mean * mean + 1e-5).sqrt()
+    for at in (0, hw // 2, hw - 4096):
+        want = (x[at:at + 4096].double().cpu() - mean) / deviation
+        assert float((y[at:at + 4096].double().cpu() - want).abs().max()) <= 1.01 * 2.0 ** -8 * float(want.abs().max()) + 1e-4
 
 
 # ---- attention -----------------------------------------------------------------------------------
