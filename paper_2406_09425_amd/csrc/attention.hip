@@ -826,8 +826,8 @@ int launch_attention(const sgprs_attention_desc_t& d, const void* q, const void*
                              d.n_seqs, d.total_q, d.total_kv, d.heads, d.kv_heads, d.heads / d.kv_heads, d.head_dim, d.causal,
                              std::fabs(d.scale) * 1.4426950408889634f, d.scale >= 0.f ? 0u : d.dtype == SGPRS_BF16 ? 0x80008000u : 0x80000000u,
                              (int)(d.ldq * es), (int)(d.ldk * es), (int)(d.ldv * es), (int)(d.ldo * es), d.hq * es, d.hk * es, d.hv * es, d.ho * es, 0, p.chunk, p.chunks, 0, p.row_blocks, nullptr, nullptr};
-    a.part_stat = (float2*)ws;
-    a.part_o = (float*)ws + 2 * (size_t)p.chunks * d.total_q * d.heads;
+    a.part_o = (float*)ws;  // first, so that its vectors of four lie on multiples of 16 bytes
+    a.part_stat = (float2*)(a.part_o + (size_t)p.chunks * d.total_q * d.heads * d.head_dim);
     return d.dtype == SGPRS_BF16 ? launch_typed<SGPRS_BF16>(a, p.decode, stream) : launch_typed<SGPRS_F32>(a, p.decode, stream);
 }
 

@@ -187,3 +187,10 @@ def test_group_norms_of_more_large_images_than_a_launch_takes(pools):
     for at in (0, 65534, 65535, 65536):
         want, bound = ref.group_norm(x[at].cpu(), None, None, None, 1, hw, groups, 1e-5, 0)
         ref.assert_within(y[at], want, bound, f"image {at} of {n}")
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("q_lens,kv_lens,heads,dim", [([1], [300], 1, 8), ([1, 1, 1], [300, 2, 129], 1, 72), ([99], [1050], 1, 40), ([35], [1100], 3, 8)], ids=str)
+def test_attention_partial_sums_of_odd_numbers_of_rows(pools, name, q_lens, kv_lens, heads, dim):
+    """Split keys where tokens, heads and chunks are odd: the vectors of partial sums keep to 16 bytes."""
+    run_attention(pools, name, q_lens, kv_lens, heads, 1, dim, True, seed=dim)
