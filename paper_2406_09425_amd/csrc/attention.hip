@@ -659,9 +659,15 @@ template <int DT, int ROWS> __global__ __launch_bounds__(256) void attention_joi
     if (n == 1) return;
     const long long step = (long long)a.total_q * a.heads;
     float* weight = weights[threadIdx.x / THREADS];
+    // what other lanes write to LDS is read behind it: a wavefront's own LDS operations run in order, as long as the compiler
+    // leaves them so
     auto meet = [] {
-        if constexpr (ROWS == 1) __syncthreads();
-        else __builtin_amdgcn_s_waitcnt(0xC07F);
+        if constexpr (ROWS == 1) {
+            __syncthreads();
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
     };
     // maximum, weights and sum
     float top = -INFINITY, total = 0.f;
