@@ -135,7 +135,7 @@ int sgprs_linear(const sgprs_linear_desc_t* d, const void* x, const void* w, con
     if (x == y || w == y) return fail(SGPRS_ERR_INVALID_ARG, "y must not alias x or w");
     if (residual == y && f.ldr != f.ldy) return fail(SGPRS_ERR_INVALID_ARG, "y on top of the residual needs the residual's stride");
     if ((rc = check_workspace(workspace, workspace_bytes, linear_workspace_bytes(f, cus)))) return rc;
-    return launch_linear(f, x, w, bias, residual, y, workspace, stream, cus);
+    return launch_linear(f, x, w, bias, residual, y, stream, cus);
 }
 
 int sgprs_group_norm_workspace(const sgprs_group_norm_desc_t* d, int partition_cus, size_t* bytes)

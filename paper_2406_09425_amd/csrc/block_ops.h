@@ -15,7 +15,7 @@ size_t linear_workspace_bytes(const sgprs_linear_desc_t& d, int cus);
 size_t group_norm_workspace_bytes(const sgprs_group_norm_desc_t& d, int cus);
 size_t attention_workspace_bytes(const sgprs_attention_desc_t& d, int cus);
 
-int launch_linear(const sgprs_linear_desc_t& d, const void* x, const void* w, const float* bias, const void* residual, void* y, void* ws,
+int launch_linear(const sgprs_linear_desc_t& d, const void* x, const void* w, const float* bias, const void* residual, void* y,
                   hipStream_t stream, int cus);
 int launch_group_norm(const sgprs_group_norm_desc_t& d, const void* x, const float* gamma, const float* beta, const void* residual, void* y,
                       void* ws, hipStream_t stream, int cus);
@@ -23,10 +23,6 @@ int launch_attention(const sgprs_attention_desc_t& d, const void* q, const void*
                      void* o, void* ws, hipStream_t stream, int cus);
 
 // ---- device side ------------------------------------------------------------
-// A tensor's element type by its dtype.
-template <int DT> struct ElemOf { typedef float type; };
-template <> struct ElemOf<SGPRS_BF16> { typedef __bf16 type; };
-
 // GELU of a bf16 result takes erf from Abramowitz and Stegun 7.1.26 (off by at most 1.5e-7): with
 // q(t) = 1 - erf(t / sqrt 2) at t = |z| it is max(z, 0) - |z| q / 2.  The library's erff took 27 us of a 69 us
 // product with 25.7 million outputs, this 2 (fp32 results keep erff).

@@ -768,7 +768,7 @@ template <int DT, bool DIRECT> static int launch_act(const LinearArgs& a, int ac
     }
 }
 
-int launch_linear(const sgprs_linear_desc_t& d, const void* x, const void* w, const float* bias, const void* residual, void* y, void* ws,
+int launch_linear(const sgprs_linear_desc_t& d, const void* x, const void* w, const float* bias, const void* residual, void* y,
                   hipStream_t stream, int cus)
 {
     const int es = (int)dtype_size(d.dtype);
