@@ -3,6 +3,7 @@ operands at the ends of fp32's range, more rows, images and sequences than a lau
 import time
 
 import pytest
+import scipy.special
 import torch
 
 import paper_2406_09425_amd as S
@@ -194,3 +195,25 @@ def test_group_norms_of_more_large_images_than_a_launch_takes(pools):
 def test_attention_partial_sums_of_odd_numbers_of_rows(pools, name, q_lens, kv_lens, heads, dim):
     """Split keys where tokens, heads and chunks are odd: the vectors of partial sums keep to 16 bytes."""
     run_attention(pools, name, q_lens, kv_lens, heads, 1, dim, True, seed=dim)
+
+
+# ---- activations ---------------------------------------------------------------------------------
+U = 2.0 ** -24
+
+
+def activation_by_scipy(z, act):
+    """z times the distribution function of a Gaussian or the logistic one, by functions that do not cancel."""
+    f = scipy.special.ndtr if act == S.SGPRS_ACT_GELU else scipy.special.expit
+    return z.double() * torch.from_numpy(f(z.double().numpy()))
+
+
+@pytest.mark.parametrize("act", [S.SGPRS_ACT_GELU, S.SGPRS_ACT_SILU], ids=["gelu", "silu"])
+@pytest.mark.parametrize("m", [24, 5000])
+def test_fp32_activations_keep_their_digits_down_the_negative_side(pools, act, m):
+    """x w^T with one input and w = 1 is x itself, so what is off is the activation.  SiLU: an exponential (2 ulp), a sum, a
+    product and a quotient, 4 u a step at most.  GELU: its argument is off by 1.5 u, of which erfc makes 2 t^2 + 1 = z^2 + 1
+    times as much, and erfc itself by 16 ulp at most.  Results below 2^-126 are multiples of 2^-149, the exponential's too."""
+    z = torch.linspace(-110.0 if act == S.SGPRS_ACT_SILU else -14.0, 12.0, m)[:, None]
+    want = activation_by_scipy(z, act)
+    relative = 16 * U if act == S.SGPRS_ACT_SILU else 2 * (z.double() ** 2 + 1) * U + 34 * U
+    ref.assert_within(linear_plain(pools, z, torch.ones(1, 1), act=act), want, relative * want.abs() + (z.double().abs() + 2) * 2.0 ** -149, f"activation {act}")
