@@ -24,7 +24,7 @@ int launch_attention(const sgprs_attention_desc_t& d, const void* q, const void*
 
 // ---- device side ------------------------------------------------------------
 // GELU of a bf16 result takes erf from Abramowitz and Stegun 7.1.26 (off by at most 1.5e-7): with
-// q(t) = 1 - erf(t / sqrt 2) at t = |z| it is max(z, 0) - |z| q / 2.  The library's erff took 27 us of a 69 us
+// q(t) = 1 - erf(t / sqrt 2) at t = |z| it is max(z, 0) - |z| q / 2 (0 z for 0: a NaN for -infinity, like the formula).  The library's erff took 27 us of a 69 us
 // product with 25.7 million outputs, this 2.  Far down the negative side, where bf16 results are below 1e-9, it is off by
 // up to 1 %.  SiLU of a bf16 result takes the approximate exponential and reciprocal (1e-6 of the result, 0 below -87).
 // fp32 results take neither: 1 + erf would cancel below z = -3 and leave no digit at -6, where erfc keeps them, and
@@ -46,7 +46,7 @@ template <int DT, int ACT> __device__ __forceinline__ float activate(float z)
             q = __builtin_fmaf(q, u, 1.421413741f);
             q = __builtin_fmaf(q, u, -0.284496736f);
             q = __builtin_fmaf(q, u, 0.254829592f) * u;
-            return (z < 0.f ? 0.f : z) - 0.5f * t * q * __builtin_amdgcn_exp2f(t * t * -0.72134752f);
+            return (z < 0.f ? 0.f * z : z) - 0.5f * t * q * __builtin_amdgcn_exp2f(t * t * -0.72134752f);
         }
         return 0.5f * z * erfcf(z * -0.70710678118654752f);
     }

@@ -217,3 +217,14 @@ def test_fp32_activations_keep_their_digits_down_the_negative_side(pools, act, m
     want = activation_by_scipy(z, act)
     relative = 16 * U if act == S.SGPRS_ACT_SILU else 2 * (z.double() ** 2 + 1) * U + 34 * U
     ref.assert_within(linear_plain(pools, z, torch.ones(1, 1), act=act), want, relative * want.abs() + (z.double().abs() + 2) * 2.0 ** -149, f"activation {act}")
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("act", [S.SGPRS_ACT_NONE, S.SGPRS_ACT_RELU, S.SGPRS_ACT_GELU, S.SGPRS_ACT_SILU], ids=["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("m", [8, 300])
+def test_activations_of_what_is_not_finite(pools, name, act, m):
+    """As the formulas say, for both types: GELU and SiLU of -infinity are -infinity times 0."""
+    z = torch.tensor([float("-inf"), float("inf"), float("nan"), -3e38, 3e38, 0.0, -1.0]).repeat(m)[:m, None].to(DT[name][1])
+    w = torch.ones(3, 1, dtype=z.dtype)
+    want, bound = ref.linear(z[:, :1].contiguous(), w, None, None, act, 0)
+    ref.assert_within(linear_plain(pools, z[:, :1].contiguous(), w, act=act), want, bound, f"activation {act} {name}")
