@@ -197,6 +197,25 @@ def test_attention_partial_sums_of_odd_numbers_of_rows(pools, name, q_lens, kv_l
     run_attention(pools, name, q_lens, kv_lens, heads, 1, dim, True, seed=dim)
 
 
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [65, 70, 4097, 4200])
+@pytest.mark.parametrize("longest,cache", [(2, 1500), (300, 1100)], ids=["tokens", "prompt"])
+def test_attention_of_more_sequences_than_a_search_step_looks_at(pools, name, n, longest, cache):
+    """64 sequences are looked at at once: two and three steps, with empty sequences, one long one and keys that are split."""
+    q_lens = torch.randint(0, 3, (n,), generator=gen(n)).tolist()
+    kv_lens = torch.randint(0, 4, (n,), generator=gen(n + 1)).tolist()
+    at = n * 2 // 3
+    q_lens[at], kv_lens[at] = longest, cache
+    run_attention(pools, name, q_lens, kv_lens, 2, 1, 32, True, seed=n, repeat=False)
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("q_lens,kv_lens,heads", [([3001], [3001], 1), ([2500, 1, 129], [2500, 2600, 4000], 2)], ids=str)
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_of_thousands_of_queries(pools, name, q_lens, kv_lens, heads, causal):
+    run_attention(pools, name, q_lens, kv_lens, heads, 1, 64, causal, seed=heads)
+
+
 # ---- activations ---------------------------------------------------------------------------------
 U = 2.0 ** -24
 
