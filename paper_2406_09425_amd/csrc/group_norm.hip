@@ -41,6 +41,17 @@ struct NormArgs {
     int chunks;              // of an image's positions
 };
 
+// 1 / sqrt(v).  The instruction takes subnormal numbers, variances of values below 2^-63, for 0.
+__device__ __forceinline__ float inverse_root(float v)
+{
+#if __HIP_DEVICE_COMPILE__
+    const bool small = v < 0x1p-100f;
+    return __builtin_amdgcn_rsqf(small ? v * 0x1p60f : v) * (small ? 0x1p30f : 1.f);
+#else
+    return v;
+#endif
+}
+
 __device__ __forceinline__ int div_magic(int m, unsigned mul, int sh) { return (int)(__umulhi(2u * (unsigned)m, mul) >> sh); }
 
 // WHOLE: the channels of every slice are whole vectors.  16-byte accesses need no alignment beyond the element's.
@@ -269,7 +280,7 @@ template <int DT, int ACT, bool WHOLE, int NV, bool FUSED> __global__ __launch_b
         for (int g = tid; g < m.groups; g += T) partial[g].y = total[g];
     } else if (m.live > 0) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) gamma[e] *= __builtin_amdgcn_rsqf(total[group[e]] * inv_count + a.eps);
+        for (int e = 0; e < V; ++e) gamma[e] *= inverse_root(total[group[e]] * inv_count + a.eps);
         unsigned char* yp = a.y + m.row0 * a.ldy + (long long)c * N::ES;
         const unsigned char* rp = a.residual + m.row0 * a.ldr + (long long)c * N::ES;
 #pragma unroll
@@ -308,7 +319,7 @@ __global__ __launch_bounds__(256) void group_norm_merge_kernel(const NormArgs a,
         m2 += one.y + (one.x - mean) * (one.x - mean) * (count(k) * (float)a.per);
     }
     m2 = all(m2, sums + 4);
-    if (tid == 0) a.merged[(long long)image * a.groups + group] = make_float2(mean, __builtin_amdgcn_rsqf(m2 * inv_hw / (float)a.per + a.eps));
+    if (tid == 0) a.merged[(long long)image * a.groups + group] = make_float2(mean, inverse_root(m2 * inv_hw / (float)a.per + a.eps));
 }
 
 // Merges an image's chunks, if that is not done, and writes the results of one of them.
@@ -355,7 +366,7 @@ template <int DT, int ACT, bool WHOLE, int NV> __global__ __launch_bounds__(1024
         m2 = lanes_sum(m2, share);
         if (g < groups && part == 0) {
             means[g] = mean;
-            scales[g] = __builtin_amdgcn_rsqf(m2 * inv_hw / (float)a.per + a.eps);
+            scales[g] = inverse_root(m2 * inv_hw / (float)a.per + a.eps);
         }
     }
     __syncthreads();
@@ -421,7 +432,7 @@ template <int DT, int ACT, bool WHOLE, int NV> __global__ __launch_bounds__(256)
                 const float t = N::get(x[k], e) - mean1;
                 sq += (WHOLE ? live[k] > 0 : e < live[k]) ? t * t : 0.f;
             }
-        const float inv = __builtin_amdgcn_rsqf(lanes_sum(sq, 64) * inv_c + a.eps);
+        const float inv = inverse_root(lanes_sum(sq, 64) * inv_c + a.eps);
         float mean[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) mean[e] = mean1;

@@ -59,6 +59,26 @@ def test_linear_of_the_largest_number_of_rows_is_refused(pools):
 
 
 @pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 49, 64, 8), (1, 12544, 64, 32), (2, 9000, 512, 4), (50, 1, 512, 1)], ids=str)
+def test_group_norms_of_tiny_values_without_eps(pools, name, shape):
+    """Deviations of 2^-66: their squares are subnormal, with 16 bits and more of those that count, so that a variance is
+    off by 2^-17 and the result by 2^-18; the bound's other parts come on top."""
+    n, hw, c, groups = shape
+    dt, tdt = DT[name]
+    x = (torch.randn(n * hw, c, generator=gen(8)) * 2.0 ** -66).to(tdt)
+    xd, y = x.cuda(), torch.zeros(n * hw, c, dtype=tdt, device="cuda")
+    d = S.GroupNormDesc(n=n, hw=hw, c=c, groups=groups, dtype=dt, eps=0.0)
+    ws_bytes = S.sgprs_group_norm_workspace(d, CUS)
+    ws = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    pool = pools()
+    S.sgprs_group_norm(d, ptr(xd), None, None, None, ptr(y), ptr(ws), ws_bytes, pool, 0)
+    pool.sync()
+    want, bound = ref.group_norm(x, None, None, None, n, hw, groups, 0.0, 0)
+    ref.assert_within(y, want, bound + 2.0 ** -16 * want.abs(), f"tiny values {shape}")
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
 @pytest.mark.parametrize("shape,cus", [((1, 12544, 256, 32), 256), ((2, 6000, 96, 3), 40), ((1, 3000, 1030, 5), 8), ((3, 4100, 64, 64), 128), ((1, 700, 4096, 4096), 256)], ids=str)
 @pytest.mark.parametrize("inplace", [None, "x", "residual"])
 def test_group_norms_of_many_chunks(pools, name, shape, cus, inplace):
