@@ -341,7 +341,7 @@ typedef struct {
     int heads, kv_heads, head_dim;  /* heads % kv_heads == 0; head_dim a multiple of 8, up to 128 */
     int dtype;                      /* of q, k, v, o */
     int causal;
-    float scale;                    /* 0: 1 / sqrt(head_dim) */
+    float scale;                    /* 0: 1 / sqrt(head_dim); up to 2e38 of either sign */
     long long ldq, ldk, ldv, ldo;   /* between tokens; 0: (kv_)heads * head_dim */
     long long hq, hk, hv, ho;       /* between heads; 0: head_dim.  (tokens first or heads first) */
 } sgprs_attention_desc_t;

@@ -72,6 +72,7 @@ int check_attention(const sgprs_attention_desc_t* d, sgprs_attention_desc_t* ful
         return fail(SGPRS_ERR_UNSUPPORTED, "more than 2^20 sequences, 65535 heads or 2^30 tokens");
     if (d->causal != 0 && d->causal != 1) return fail(SGPRS_ERR_INVALID_ARG, "causal %d is neither 0 nor 1", d->causal);
     if (!(d->scale > -3e38f && d->scale < 3e38f)) return fail(SGPRS_ERR_INVALID_ARG, "scale is not finite");
+    if (d->scale < -2e38f || d->scale > 2e38f) return fail(SGPRS_ERR_UNSUPPORTED, "scale %g: supported is up to 2e38 of either sign", (double)d->scale);  // times log2 e
     *full = *d;
     if (d->scale == 0.f) full->scale = 1.f / sqrtf((float)d->head_dim);
     const int vec = 16 / (int)dtype_size(d->dtype);

@@ -16,6 +16,17 @@ def test_group_norm_of_the_largest_number_of_positions():
     assert INT_MAX // 65536 * 8 <= need <= INT_MAX // 256 * 8
 
 
+@pytest.mark.parametrize("scale,fine", [(2e38, True), (-2e38, True), (2.4e38, False), (-2.9e38, False)])
+def test_attention_scales_stay_finite_in_base_2(scale, fine):
+    d = S.AttentionDesc(n_seqs=1, total_q=1, total_kv=1, max_q=1, max_kv=1, heads=1, kv_heads=1, head_dim=8, dtype=S.SGPRS_F32, scale=scale)
+    if fine:
+        assert S.sgprs_attention_workspace(d, 256) == 0
+    else:
+        with pytest.raises(S.SgprsError) as e:
+            S.sgprs_attention_workspace(d, 256)
+        assert e.value.status == -5
+
+
 def test_lanes_of_a_join_meet_before_they_read_each_others_weights(tmp_path):
     """A wavefront per row: nothing but the fences holds its LDS writes and reads in their order."""
     found = {n: t for n, t in kernels(tmp_path, "attention.hip", "attention_join_kernel").items() if "ELi4E" in n}
