@@ -268,7 +268,8 @@ int sgprs_avgpool_fc_static(int dtype, int n, int hw, int cin, int cout, const v
  * transformer layer, for networks that run beside the convolutional ones:
  * token- or pixel-wise products, a norm whose statistics are the input's own,
  * and attention.  Both dtypes; sums, statistics and softmax in fp32, results
- * rounded once on store.
+ * rounded once on store (bf16 attention also rounds the weights to bf16, for
+ * their product with v; their sum takes them unrounded).
  *
  * Strides count elements; 0 stands for the dense value.  Rows may start at any
  * multiple of the element size; where pointers are 16-byte aligned and strides

@@ -168,7 +168,9 @@ template <int HD> __device__ __forceinline__ u32x4_t value_fragment(unsigned v_b
     return f;
 }
 
-// o += V^T P^T for one block of 32 keys; p: this lane's 16 weights.  CLEAN: some keys are not seen, and where v holds
+// o += V^T P^T for one block of 32 keys; p: this lane's 16 weights.  bf16: they are rounded to bf16, as the matrix cores
+// take them beside v (their sum is of the fp32 ones); errors of a result rise from 1.6e-3, its own rounding, to 2.1e-3,
+// where weights in two parts would double the products with v.  CLEAN: some keys are not seen, and where v holds
 // infinities or NaNs 0 * v would be NaN: such values are left out (*odd: there are some) for add_not_finite.
 template <int DT, int HD, bool CLEAN>
 __device__ __forceinline__ void add_values(f32x16_t* o, const float* p, unsigned v_base, int block, bool* odd)
@@ -394,7 +396,7 @@ __device__ __forceinline__ int chunks_of(const AttentionArgs& a, int query, int 
 // 128 queries of one head per workgroup, 32 per wavefront; tiles of keys in an LDS ring of two or three stages.
 // bf16: bound by the vector units' softmax and what the two (heads of 64: three) wavefronts of a SIMD cannot hide of it
 // behind each other's MFMAs: heads of 128, 59 % of their time and 35 % of the matrix cores'; 2 x 4096 tokens, 16 heads of
-// 128: 322 us, 855 TFLOP/s; 8192 tokens, 16 heads of 64: 356 us, 772.  fp32 by fp32 MFMAs: 4 x 1024 tokens, 8 heads of
+// 128: 321 us, 857 TFLOP/s; 8192 tokens, 16 heads of 64: 362 us, 759.  fp32 by fp32 MFMAs: 4 x 1024 tokens, 8 heads of
 // 128: 170 us, 101 TFLOP/s.  Registers decide: what the compiler would keep of addresses and masks is worked out in every
 // tile, since one spilled register waits for all keys on their way (heads of 128: 714 -> 849 TFLOP/s).
 template <int DT, int HD> struct PromptShape {

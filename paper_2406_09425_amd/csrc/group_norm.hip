@@ -9,9 +9,9 @@
 //     workspace) and one that merges an image's chunks and writes the results; with many chunks, which every
 //     workgroup would have to read, a launch between the two merges them;
 //   * a norm over all channels of single positions (layer norm) is a wavefront per row.
-// 64 images of 112 x 112 x 64 bf16 with residual and SiLU: 88 us, 26 of them statistics (x once, 4 TB/s) and 62 results
-// (x from the caches, residual, y: 4.9 TB/s, what a copy reaches).  12544 layer norms of 512 bf16 channels 6.6 us
-// (3.9 TB/s; a plain copy of as much 5); one map of 49 positions 3.8 us, a launch.
+// 64 images of 112 x 112 x 64 bf16 with residual and SiLU: 79 us, of launches of 19 (statistics, x once, 5.4 TB/s), 5 (the
+// chunks) and 48 (results: x from the caches, residual, y, 6.4 TB/s).  12544 layer norms of 512 bf16 channels 6.6 us
+// (3.9 TB/s; a copy of as much 4.2 at the rate of larger ones, 5 by itself); one map of 49 positions 3.6 to 4.2 us, a launch.
 #include <algorithm>
 #include <type_traits>
 

@@ -228,10 +228,10 @@ __device__ __forceinline__ void tile_of(int id, int grid_m, int grid_n, int* tm,
 // BM x BN outputs, 2 x 2 wavefronts; two k-tiles in LDS, filled by loads that write it directly.  The barrier of a
 // k-tile stands between its two halves: before it the second half's fragments have been read, so that its MFMAs
 // follow the barrier at once while the next k-tile's first fragments are read and the one after that is requested
-// into the buffer just left, a load behind every fourth MFMA (twice as fast: 447 us instead of 409 below).
+// into the buffer just left, a load behind every fourth MFMA (one behind every second one: 447 us instead of 409).
 // Bound by the matrix cores at the clock they leave: 256 x 256 (one wavefront a SIMD, 256 accumulators; half the LDS
-// reads per MFMA of 128 x 128) keeps them 68 % busy at 1.9 GHz, 16384x4096 -> 4096 in 409 us, 1343 TFLOP/s, where a
-// large library product reaches 1529.  128 x 128 (two workgroups a CU) is for what 256 x 256 divides badly: a tile's
+// reads per MFMA of 128 x 128) keeps them 70 % busy at 1.9 GHz, 16384x4096 -> 4096 in 409 to 415 us by card, 1343 to
+// 1325 TFLOP/s (with a residual 420 to 424), where a large library product reaches 1529 to 1546.  128 x 128 (two workgroups a CU) is for what 256 x 256 divides badly: a tile's
 // beginning and end cost as much as five k-tiles.
 template <int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM * BN >= 256 * 128 ? 1 : 2) void linear_tile_kernel(const LinearArgs a)
 {
@@ -337,11 +337,11 @@ template <int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM * BN >= 
 // number, 2^-149 times ordinary values was off by 2^-17).  A sum that is not finite then (infinities have no such parts;
 // operands from 2^104 and sums from 2^80 on pass the range) sends its wavefront through the fp32 matrix cores, with the
 // operands as they are.
-// 128 x 128, fp32: bound by the splitting (half of the vector units' time) and the MFMAs, 4096x4096 -> 4096 in 680 us,
-// 200 TFLOP/s; fp32 MFMAs on the same tiles reached 142, the rate of the fp32 matrix cores is 157.  Relative error
+// 128 x 128, fp32: bound by the splitting (half of the vector units' time) and the MFMAs, 4096x4096 -> 4096 in 700 us,
+// 196 TFLOP/s (17 us of it the scaling); fp32 MFMAs on the same tiles reached 142, the rate of the fp32 matrix cores is 157.  Relative error
 // against 64 bits 1.6e-7 (plain fp32 chains 2.9e-7 to 7e-7).  64 x 64 with two groups of wavefronts that take every
 // other k-tile is for fewer tiles: the second group covers what the first one waits for (fp32 300x700 -> 700 19.9 -> 16.8,
-// 3136x512 -> 512 19.8 -> 17.4 us).
+// 3136x512 -> 512 19.8 -> 17.5 us).
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ unsigned pack_bf16x2(float lo, float hi)
 {
@@ -701,7 +701,7 @@ size_t linear_workspace_bytes(const sgprs_linear_desc_t&, int) { return 0; }
 // 12544x512 -> 2048 46 / 42 / 52, 16384x512 -> 512 - / 15.1 / 20.9, 3136x512 -> 512 - / 9.3 / 7.0 (K split over wavefronts
 // 21); 300x700 -> 700 18 / 7.2 / 7.6 for 128 x 128 / 64 x 64 / K split.  fp32, 128 x 128 / 64 x 64 / K split:
 // 4096x4096 -> 4096 677 / 894 / 1213, 16384x512 -> 512 55 / 71 / 140, 1000x1024 -> 1024 66 / 22 / 28, 300x700 -> 700
-// 45 / 17 / 7.2.
+// 45 / 17 / 7.2 (before the operands' scaling, which adds up to 3 % to the first two).
 static int plan_linear(const sgprs_linear_desc_t& d, int cus, bool direct)
 {
     auto tiles = [&](int b, int c) { return (double)((d.m + (long long)b - 1) / b) * ((d.n + c - 1) / c); };
