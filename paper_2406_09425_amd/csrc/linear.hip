@@ -7,17 +7,14 @@
 // four k groups take elements 4 g + s, for both operands alike, so the order within a k-tile is all that changes).
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
-#include <utility>
 
-#include "block_ops.h"
+#include "linear_tiles.h"
 
 namespace sgprs {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
-typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 
 struct LinearArgs {
     const unsigned char* x;
@@ -30,8 +27,6 @@ struct LinearArgs {
     int residual_first;
     int grid_m, grid_n;      // tiles
 };
-
-constexpr unsigned kOutside = 0x80000000u;  // beyond any descriptor's size: reads zeros
 
 template <int DT> __device__ __forceinline__ f32x4_t mma(u32x4_t a, u32x4_t b, f32x4_t c)
 {
@@ -66,23 +61,6 @@ template <int N, int M> __device__ __forceinline__ void settle(f32x4_t (&acc)[N]
 #pragma unroll
         for (int i = 0; i < M; ++i) asm volatile("" : "+a"(acc[j][i]));
 #endif
-}
-
-// 16 bytes at any alignment, of which the first `bytes` (a multiple of ES, may be <= 0) exist; zeros for the others.
-template <int ES> __device__ __forceinline__ u32x4_t load_chunk(const unsigned char* p, int bytes)
-{
-    u32x4_t v = {0, 0, 0, 0};
-    if (bytes >= 16) {
-        __builtin_memcpy(&v, p, 16);
-    } else if (bytes > 0) {
-#pragma unroll
-        for (int e = 0; e < 16 / ES; ++e) {
-            if (e * ES >= bytes) continue;
-            if constexpr (ES == 2) v[e / 2] |= (unsigned)*(const unsigned short*)(p + e * 2) << (e % 2 * 16);
-            else v[e] = *(const unsigned*)(p + e * 4);
-        }
-    }
-    return v;
 }
 
 // Eight (bf16) or four (fp32) neighbouring outputs of one row.  z: the sums, r: the residual as it lies in memory.
@@ -139,23 +117,12 @@ template <int V> __device__ __forceinline__ void load_bias(const LinearArgs& a, 
     for (int e = 0; e < V; ++e) bias[e] = a.bias && col + e < a.n ? a.bias[col + e] : 0.f;
 }
 
-#if __HIP_DEVICE_COMPILE__
-typedef __attribute__((address_space(3))) void* lds_ptr_t;
-typedef __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
-__device__ __forceinline__ u32x4_t lds_read(unsigned at) { return *(const lds_u32x4_t*)(unsigned long)at; }
-#endif
-
 // A wavefront's 16 TM x 16 TN outputs, from row m0 and column n0 on: 16 rows at a time through LDS of its own (`mine`),
 // then V neighbouring outputs a lane.
 template <int DT, int TN> struct StagedRows {
     static constexpr int V = DT == SGPRS_BF16 ? 8 : 4, PITCH = TN * 16 + 4;  // floats of a staged row
     static constexpr int BYTES = 16 * PITCH * 4;
 };
-// for_each<N>(f): f(0), ..., f(N - 1) as constants.  (A loop over accumulators that the compiler finds too long to unroll
-// would put them in memory.)
-template <class F, int... I> __device__ __forceinline__ void for_each(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
-template <int N, class F> __device__ __forceinline__ void for_each(F f) { for_each(f, std::make_integer_sequence<int, N>()); }
-
 template <int DT, int ACT, int TM, int TN>
 __device__ __forceinline__ void store_tile(const LinearArgs& a, const f32x4_t (&acc)[TN][TM], float* mine, long long m0, int n0)
 {
@@ -211,17 +178,6 @@ __device__ __forceinline__ void store_tile(const LinearArgs& a, const f32x4_t (&
         });
     }
 #endif
-}
-
-// Tile of workgroup `id`: workgroups are dealt to the eight dies in turn; each die gets a run of consecutive
-// tiles, walked in bands of eight row tiles, so that what a die works on at once shares operands in its L2.
-__device__ __forceinline__ void tile_of(int id, int grid_m, int grid_n, int* tm, int* tn)
-{
-    const int tiles = grid_m * grid_n, per = tiles >> 3, rest = tiles & 7, die = id & 7;
-    const int t = die * per + min(die, rest) + (id >> 3);
-    const int band = t / (8 * grid_n), in = t - band * 8 * grid_n, rows = min(8, grid_m - band * 8);
-    *tn = in / rows;
-    *tm = band * 8 + in - *tn * rows;
 }
 
 // ---- tiles shared by a workgroup: aligned bf16 --------------------------------------------------
