@@ -45,7 +45,11 @@ extern "C" {
 typedef struct sgprs_pool sgprs_pool_t;
 typedef struct sgprs_task sgprs_task_t;
 
-typedef enum { SGPRS_F32 = 0, SGPRS_BF16 = 1 } sgprs_dtype_t;
+typedef enum {
+    SGPRS_F32 = 0,
+    SGPRS_BF16 = 1,
+    SGPRS_I8 = 2 /* only where an operator says so (sgprs_rms_norm's out_dtype) */
+} sgprs_dtype_t;
 
 enum {
     SGPRS_OK = 0,
@@ -356,6 +360,131 @@ int sgprs_attention_workspace(const sgprs_attention_desc_t *d, int partition_cus
 int sgprs_attention(const sgprs_attention_desc_t *d, const void *q, const void *k, const void *v,
                     const int *q_offsets, const int *kv_offsets, void *o, void *workspace,
                     size_t workspace_bytes, sgprs_pool_t *pool, int partition);
+
+/* ------------------------------------------------------ decoding steps ----
+ * The operators of a decoder's step for one new token of each of many sequences
+ * (or a batch of prompts), with 8-bit products and a cache of pages:
+ *
+ *   sgprs_rms_norm (x + residual, 8-bit)  ->  sgprs_linear_i8 (q, k, v)
+ *   ->  sgprs_paged_append (k, v)  ->  sgprs_paged_attention (q)
+ *   ->  sgprs_quantize_i8  ->  sgprs_linear_i8  ->  ...
+ *
+ * Strides, alignment, empty calls and overlaps are as for attention blocks.
+ * Statistics, sums and softmax are held in 32 bits or more; products of 8-bit
+ * integers are summed exactly.
+ *
+ * 8-bit rows: a row t of c values is held as integers q and a scale, t ~ q scale,
+ *   q = nearest integer (ties to even) of 127 t / max|t|,   scale = max|t| / 127
+ * where the quotient is the one of 64-bit arithmetic, (127 t) / max|t|: the integers do not
+ * depend on how a call is planned.  A row of zeros has q = 0, scale = 0; a row
+ * that holds an infinity or a NaN has q = 0, scale = NaN, so that products with
+ * it are NaN. */
+
+/* h = x (+ residual), rounded to the dtype, and of a row h, as it is rounded,
+ *   y = h * gamma / sqrt( mean(h^2) + eps )
+ * in the dtype, or as 8-bit rows (out_dtype SGPRS_I8).  With eps = 0 a row of
+ * zeros gives NaN (0 / 0).  No square overflows or vanishes, whatever the row's size. */
+typedef struct {
+    int m, c;                       /* rows, channels */
+    int dtype;                      /* of x, residual, sum, and of y unless it is 8-bit */
+    int out_dtype;                  /* dtype or SGPRS_I8 */
+    float eps;                      /* >= 0 */
+    long long ldx, ldr, ldh, ldy;   /* between rows of x, residual, sum, y; 0: c */
+} sgprs_rms_norm_desc_t;
+/* x, residual (may be NULL), y DEVICE; gamma NULL (1) or DEVICE fp32[c]; sum:
+ * where h goes, NULL if it is not wanted, and without a residual; scales: DEVICE fp32[m]
+ * for 8-bit rows, else NULL.  sum may be x or the residual, and so may y (in the
+ * dtype) where it is not sum (same pointer and stride).  Needs no workspace. */
+int sgprs_rms_norm(const sgprs_rms_norm_desc_t *d, const void *x, const void *residual,
+                   const float *gamma, void *sum, void *y, float *scales, sgprs_pool_t *pool,
+                   int partition);
+
+/* Rows of x as 8-bit rows: activations that no norm precedes, and weights (a row
+ * for each output channel), once. */
+typedef struct {
+    int m, c;
+    int dtype;                      /* of x */
+    long long ldx, ldy;             /* between rows; 0: c */
+} sgprs_quantize_desc_t;
+/* x [m][c], y int8 [m][c], scales fp32[m] DEVICE. */
+int sgprs_quantize_i8(const sgprs_quantize_desc_t *d, const void *x, int8_t *y, float *scales,
+                      sgprs_pool_t *pool, int partition);
+
+/* y[i][j] = act( x_scales[i] w_scales[j] sum_k x[i][k] w[j][k] + bias[j] ) + residual[i][j],
+ * or, with residual_first, act( ... + residual ).  The sum is exact; it is
+ * multiplied by the row's scale first, then the channel's.  UNSUPPORTED: k over
+ * 131071, where a sum could pass 32 bits. */
+typedef struct {
+    int m, n, k;                    /* rows of x, outputs, inputs */
+    int dtype;                      /* sgprs_dtype_t of residual and y */
+    int act;                        /* sgprs_act_t */
+    int residual_first;             /* 1: the residual is added before the activation */
+    long long ldx, ldw, ldr, ldy;   /* between rows; 0: k, k, n, n */
+} sgprs_linear_i8_desc_t;
+int sgprs_linear_i8_workspace(const sgprs_linear_i8_desc_t *d, int partition_cus, size_t *bytes);
+/* x int8 [m][k], w int8 [n][k] (any values, -128 too), residual NULL or [m][n],
+ * y [m][n] DEVICE; x_scales NULL (1) or fp32[m], w_scales NULL (1) or fp32[n],
+ * bias NULL or fp32[n] DEVICE.  y may be the residual (same pointer and stride).
+ * Fastest where x, w and their strides are multiples of 16 bytes. */
+int sgprs_linear_i8(const sgprs_linear_i8_desc_t *d, const int8_t *x, const float *x_scales,
+                    const int8_t *w, const float *w_scales, const float *bias, const void *residual,
+                    void *y, void *workspace, size_t workspace_bytes, sgprs_pool_t *pool,
+                    int partition);
+
+/* A cache of pages: n_pages pages of page_size positions of kv_heads rows of
+ * head_dim values, one buffer for keys and one of the same layout for values.
+ * Position p of sequence s lies in page table[s * table_width + p / page_size],
+ * at position p % page_size of it.  Entries are read for positions that the call
+ * needs, and no others.  kv_lens, table and offsets are read by the kernels, so
+ * their values cannot be refused: a length beyond table_width * page_size (or
+ * negative) counts as the nearest possible one, what would go to a page outside
+ * 0 .. n_pages - 1 is not written, and what is read from there is unspecified, but nothing
+ * outside the tensors is read or written. */
+
+/* The new keys and values of n_seqs sequences to their places in the cache: they
+ * are the last ones of the kv_lens[s] positions that sequence s has with them.
+ * Tokens offsets[s] .. offsets[s+1]-1 of k and v belong to sequence s (offsets
+ * NULL: token s does, one for each).  A token whose position would be negative, as where kv_lens[s] is
+ * 0, goes nowhere.  If a place is written twice, either may be there. */
+typedef struct {
+    int n_seqs, total;              /* sequences, tokens in k and v */
+    int kv_heads, head_dim;         /* head_dim a multiple of 8, up to 128 */
+    int dtype;
+    int n_pages, page_size, table_width;
+    long long ldk, ldv, hk, hv;     /* of k, v between tokens and heads; 0: kv_heads * head_dim, head_dim */
+    long long page_stride, token_stride, head_stride; /* of the cache; 0: page_size * kv_heads * head_dim,
+                                       kv_heads * head_dim, head_dim.  Places must not overlap */
+} sgprs_paged_append_desc_t;
+/* k, v, caches DEVICE in dtype, 16-byte aligned, strides multiples of 16 bytes; offsets DEVICE
+ * int32[n_seqs + 1] or NULL, table DEVICE int32[n_seqs][table_width], kv_lens DEVICE int32[n_seqs]. */
+int sgprs_paged_append(const sgprs_paged_append_desc_t *d, const void *k, const void *v,
+                       const int *offsets, const int *table, const int *kv_lens, void *k_cache,
+                       void *v_cache, sgprs_pool_t *pool, int partition);
+
+/* Attention of one new token of each sequence over its pages: query head h reads
+ * key head h / (heads / kv_heads),
+ *   o = sum_j p_j v_j,  p = softmax_j( scale * q . k_j )
+ * over positions j < kv_lens[s] of the sequence (its own key among them, appended
+ * before); with a window, over the last `window` of them and the first `sinks`.
+ * A sequence without a position gets zeros; positions that are not seen are not
+ * read.  bf16 rounds as sgprs_attention does. */
+typedef struct {
+    int n_seqs;
+    int heads, kv_heads, head_dim;  /* heads % kv_heads == 0; head_dim a multiple of 8, up to 128 */
+    int dtype;                      /* of q, caches, o */
+    int n_pages, page_size, table_width;
+    int window, sinks;              /* 0: all positions; sinks need a window */
+    float scale;                    /* 0: 1 / sqrt(head_dim); up to 2e38 of either sign */
+    long long ldq, ldo, hq, ho;     /* between tokens and heads; 0: heads * head_dim, head_dim */
+    long long page_stride, token_stride, head_stride; /* as for sgprs_paged_append */
+} sgprs_paged_attention_desc_t;
+int sgprs_paged_attention_workspace(const sgprs_paged_attention_desc_t *d, int partition_cus,
+                                    size_t *bytes);
+/* As above; q, o [n_seqs][heads][head_dim].  The work is divided by the lengths that
+ * the kernels find, so a captured call stays balanced when they change. */
+int sgprs_paged_attention(const sgprs_paged_attention_desc_t *d, const void *q, const void *k_cache,
+                          const void *v_cache, const int *table, const int *kv_lens, void *o,
+                          void *workspace, size_t workspace_bytes, sgprs_pool_t *pool, int partition);
 
 /* ------------------------------------------------------------------ task --
  * Task tau_i = one ResNet18 instance, split into the paper's six stages:

@@ -25,9 +25,12 @@ __all__ = [
     "SGPRS_ACT_NONE", "SGPRS_ACT_RELU", "SGPRS_ACT_GELU", "SGPRS_ACT_SILU", "LinearDesc", "GroupNormDesc", "AttentionDesc",
     "sgprs_linear_workspace", "sgprs_linear", "sgprs_group_norm_workspace", "sgprs_group_norm", "sgprs_attention_workspace",
     "sgprs_attention",
+    "SGPRS_I8", "RmsNormDesc", "QuantizeDesc", "LinearI8Desc", "PagedAppendDesc", "PagedAttentionDesc",
+    "sgprs_rms_norm", "sgprs_quantize_i8", "sgprs_linear_i8_workspace", "sgprs_linear_i8", "sgprs_paged_append",
+    "sgprs_paged_attention_workspace", "sgprs_paged_attention",
 ]
 
-SGPRS_F32, SGPRS_BF16 = 0, 1
+SGPRS_F32, SGPRS_BF16, SGPRS_I8 = 0, 1, 2
 SGPRS_POOL_OVERSUBSCRIBE, SGPRS_POOL_BLOCKED_LAYOUT = 1, 2
 SGPRS_ACT_NONE, SGPRS_ACT_RELU, SGPRS_ACT_GELU, SGPRS_ACT_SILU = 0, 1, 2, 3
 ERR_NAMES = {-1: "INVALID_ARG", -2: "NO_DEVICE", -3: "HIP", -4: "OOM", -5: "UNSUPPORTED", -6: "OVERSUBSCRIBED"}
@@ -59,6 +62,31 @@ class AttentionDesc(ctypes.Structure):
     _fields_ = [(n, c_int) for n in ("n_seqs", "total_q", "total_kv", "max_q", "max_kv", "heads", "kv_heads", "head_dim", "dtype",
                                      "causal")] + [("scale", c_float)] + \
                [(n, c_longlong) for n in ("ldq", "ldk", "ldv", "ldo", "hq", "hk", "hv", "ho")]
+
+
+class RmsNormDesc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("m", "c", "dtype", "out_dtype")] + [("eps", c_float)] + \
+               [(n, c_longlong) for n in ("ldx", "ldr", "ldh", "ldy")]
+
+
+class QuantizeDesc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("m", "c", "dtype")] + [(n, c_longlong) for n in ("ldx", "ldy")]
+
+
+class LinearI8Desc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("m", "n", "k", "dtype", "act", "residual_first")] + \
+               [(n, c_longlong) for n in ("ldx", "ldw", "ldr", "ldy")]
+
+
+class PagedAppendDesc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("n_seqs", "total", "kv_heads", "head_dim", "dtype", "n_pages", "page_size", "table_width")] + \
+               [(n, c_longlong) for n in ("ldk", "ldv", "hk", "hv", "page_stride", "token_stride", "head_stride")]
+
+
+class PagedAttentionDesc(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("n_seqs", "heads", "kv_heads", "head_dim", "dtype", "n_pages", "page_size", "table_width",
+                                     "window", "sinks")] + [("scale", c_float)] + \
+               [(n, c_longlong) for n in ("ldq", "ldo", "hq", "ho", "page_stride", "token_stride", "head_stride")]
 
 
 class _Params(ctypes.Structure):
@@ -141,6 +169,13 @@ def lib():
         "sgprs_group_norm": (c_int, [POINTER(GroupNormDesc), vp, vp, vp, vp, vp, vp, c_size_t, vp, c_int]),
         "sgprs_attention_workspace": (c_int, [POINTER(AttentionDesc), c_int, POINTER(c_size_t)]),
         "sgprs_attention": (c_int, [POINTER(AttentionDesc), vp, vp, vp, vp, vp, vp, vp, c_size_t, vp, c_int]),
+        "sgprs_rms_norm": (c_int, [POINTER(RmsNormDesc), vp, vp, vp, vp, vp, vp, vp, c_int]),
+        "sgprs_quantize_i8": (c_int, [POINTER(QuantizeDesc), vp, vp, vp, vp, c_int]),
+        "sgprs_linear_i8_workspace": (c_int, [POINTER(LinearI8Desc), c_int, POINTER(c_size_t)]),
+        "sgprs_linear_i8": (c_int, [POINTER(LinearI8Desc), vp, vp, vp, vp, vp, vp, vp, vp, c_size_t, vp, c_int]),
+        "sgprs_paged_append": (c_int, [POINTER(PagedAppendDesc), vp, vp, vp, vp, vp, vp, vp, vp, c_int]),
+        "sgprs_paged_attention_workspace": (c_int, [POINTER(PagedAttentionDesc), c_int, POINTER(c_size_t)]),
+        "sgprs_paged_attention": (c_int, [POINTER(PagedAttentionDesc), vp, vp, vp, vp, vp, vp, vp, c_size_t, vp, c_int]),
         "sgprs_task_create_resnet18": (c_int, [c_int, c_int, c_int, POINTER(_Params), POINTER(vp)]),
         "sgprs_task_destroy": (c_int, [vp]),
         "sgprs_task_num_stages": (c_int, [vp]),
@@ -469,6 +504,73 @@ def sgprs_attention(desc: AttentionDesc, q: int, k: int, v: int, q_offsets: int,
                                              pool.address if pool.__class__ is Pool else _address(_h(pool)), partition)
     if rc is None:
         rc = lib().sgprs_attention(ctypes.byref(desc), q, k, v, q_offsets, kv_offsets, o, workspace, workspace_bytes, _h(pool), partition)
+    if rc:
+        _check(rc)
+
+
+def sgprs_rms_norm(desc: RmsNormDesc, x: int, residual: int | None, gamma: int | None, sum: int | None, y: int, scales: int | None, pool,
+                   partition: int) -> None:
+    rc = None
+    if desc.__class__ is RmsNormDesc:
+        rc = (_native or _calls()).rms_norm(ctypes.addressof(desc), x, residual, gamma, sum, y, scales,
+                                          pool.address if pool.__class__ is Pool else _address(_h(pool)), partition)
+    if rc is None:
+        rc = lib().sgprs_rms_norm(ctypes.byref(desc), x, residual, gamma, sum, y, scales, _h(pool), partition)
+    if rc:
+        _check(rc)
+
+
+def sgprs_quantize_i8(desc: QuantizeDesc, x: int, y: int, scales: int, pool, partition: int) -> None:
+    rc = None
+    if desc.__class__ is QuantizeDesc:
+        rc = (_native or _calls()).quantize_i8(ctypes.addressof(desc), x, y, scales,
+                                          pool.address if pool.__class__ is Pool else _address(_h(pool)), partition)
+    if rc is None:
+        rc = lib().sgprs_quantize_i8(ctypes.byref(desc), x, y, scales, _h(pool), partition)
+    if rc:
+        _check(rc)
+
+
+def sgprs_linear_i8_workspace(desc: LinearI8Desc, partition_cus: int) -> int:
+    return _workspace(lib().sgprs_linear_i8_workspace, desc, partition_cus)
+
+
+def sgprs_linear_i8(desc: LinearI8Desc, x: int, x_scales: int | None, w: int, w_scales: int | None, bias: int | None, residual: int | None,
+                    y: int, workspace: int | None, workspace_bytes: int, pool, partition: int) -> None:
+    rc = None
+    if desc.__class__ is LinearI8Desc:
+        rc = (_native or _calls()).linear_i8(ctypes.addressof(desc), x, x_scales, w, w_scales, bias, residual, y, workspace, workspace_bytes,
+                                          pool.address if pool.__class__ is Pool else _address(_h(pool)), partition)
+    if rc is None:
+        rc = lib().sgprs_linear_i8(ctypes.byref(desc), x, x_scales, w, w_scales, bias, residual, y, workspace, workspace_bytes, _h(pool), partition)
+    if rc:
+        _check(rc)
+
+
+def sgprs_paged_append(desc: PagedAppendDesc, k: int, v: int, offsets: int | None, table: int, kv_lens: int, k_cache: int, v_cache: int,
+                       pool, partition: int) -> None:
+    rc = None
+    if desc.__class__ is PagedAppendDesc:
+        rc = (_native or _calls()).paged_append(ctypes.addressof(desc), k, v, offsets, table, kv_lens, k_cache, v_cache,
+                                          pool.address if pool.__class__ is Pool else _address(_h(pool)), partition)
+    if rc is None:
+        rc = lib().sgprs_paged_append(ctypes.byref(desc), k, v, offsets, table, kv_lens, k_cache, v_cache, _h(pool), partition)
+    if rc:
+        _check(rc)
+
+
+def sgprs_paged_attention_workspace(desc: PagedAttentionDesc, partition_cus: int) -> int:
+    return _workspace(lib().sgprs_paged_attention_workspace, desc, partition_cus)
+
+
+def sgprs_paged_attention(desc: PagedAttentionDesc, q: int, k_cache: int, v_cache: int, table: int, kv_lens: int, o: int,
+                          workspace: int | None, workspace_bytes: int, pool, partition: int) -> None:
+    rc = None
+    if desc.__class__ is PagedAttentionDesc:
+        rc = (_native or _calls()).paged_attention(ctypes.addressof(desc), q, k_cache, v_cache, table, kv_lens, o, workspace, workspace_bytes,
+                                          pool.address if pool.__class__ is Pool else _address(_h(pool)), partition)
+    if rc is None:
+        rc = lib().sgprs_paged_attention(ctypes.byref(desc), q, k_cache, v_cache, table, kv_lens, o, workspace, workspace_bytes, _h(pool), partition)
     if rc:
         _check(rc)
 

@@ -7,10 +7,8 @@
 
 namespace sgprs {
 
-constexpr long long kMaxStride = 1 << 20;  // elements between rows: a tile's rows are addressed with 32-bit byte offsets
-
 // Fills in the dense value; the row must hold `width` elements.
-static int fill_stride(const char* name, long long* ld, long long width)
+int fill_stride(const char* name, long long* ld, long long width)
 {
     if (*ld == 0) *ld = width;
     if (*ld < width) return fail(SGPRS_ERR_INVALID_ARG, "%s %lld is less than the %lld elements of a row", name, *ld, width);
@@ -18,7 +16,7 @@ static int fill_stride(const char* name, long long* ld, long long width)
     return SGPRS_OK;
 }
 
-static int check_kind(int dtype, int act)
+int check_kind(int dtype, int act)
 {
     if (!dtype_ok(dtype)) return fail(SGPRS_ERR_UNSUPPORTED, "dtype %d", dtype);
     if (act < SGPRS_ACT_NONE || act > SGPRS_ACT_SILU) return fail(SGPRS_ERR_UNSUPPORTED, "activation %d", act);
@@ -91,15 +89,13 @@ int check_attention(const sgprs_attention_desc_t* d, sgprs_attention_desc_t* ful
     return SGPRS_OK;
 }
 
-static bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
-
-static int check_cus(int cus, const size_t* bytes)
+int check_cus(int cus, const size_t* bytes)
 {
     if (cus <= 0 || cus > SGPRS_MAX_MASK_WORDS * 32 || !bytes) return fail(SGPRS_ERR_INVALID_ARG, "partition of %d CUs, or NULL result pointer", cus);
     return SGPRS_OK;
 }
 
-static int check_workspace(const void* ws, size_t have, size_t need)
+int check_workspace(const void* ws, size_t have, size_t need)
 {
     if (need && (!ws || have < need || !aligned(ws, 16)))
         return fail(SGPRS_ERR_INVALID_ARG, "workspace of %zu bytes: %zu are needed, 16-byte aligned", ws ? have : (size_t)0, need);

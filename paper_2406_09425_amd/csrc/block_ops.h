@@ -5,6 +5,15 @@
 
 namespace sgprs {
 
+constexpr long long kMaxStride = 1 << 20;  // elements between rows: a tile's rows are addressed with 32-bit byte offsets
+
+// Checks that the operators' entry points share; 0 or the error that the call returns.
+int fill_stride(const char* name, long long* ld, long long width);
+int check_kind(int dtype, int act);
+int check_cus(int cus, const size_t* bytes);
+int check_workspace(const void* ws, size_t have, size_t need);
+inline bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
 // Descriptors with the dense strides filled in and everything checked.
 int check_linear(const sgprs_linear_desc_t* d, sgprs_linear_desc_t* full);
 int check_group_norm(const sgprs_group_norm_desc_t* d, sgprs_group_norm_desc_t* full);

@@ -73,6 +73,20 @@ METHOD(group_norm, 10, auto* d = a.p<sgprs_group_norm_desc_t>(); auto* x = a.p()
 METHOD(attention, 11, auto* d = a.p<sgprs_attention_desc_t>(); auto* q = a.p(); auto* k = a.p(); auto* v = a.p(); auto* qo = a.p<int>();
        auto* ko = a.p<int>(); auto* o = a.p(); auto* ws = a.p(); size_t wb = a.z(); auto* pool = a.p<sgprs_pool_t>(); int part = a.i(),
        sgprs_attention(d, q, k, v, qo, ko, o, ws, wb, pool, part))
+METHOD(rms_norm, 9, auto* d = a.p<sgprs_rms_norm_desc_t>(); auto* x = a.p(); auto* res = a.p(); auto* ga = a.p<float>(); auto* sum = a.p();
+       auto* y = a.p(); auto* sc = a.p<float>(); auto* pool = a.p<sgprs_pool_t>(); int part = a.i(),
+       sgprs_rms_norm(d, x, res, ga, sum, y, sc, pool, part))
+METHOD(quantize_i8, 6, auto* d = a.p<sgprs_quantize_desc_t>(); auto* x = a.p(); auto* y = a.p<int8_t>(); auto* sc = a.p<float>();
+       auto* pool = a.p<sgprs_pool_t>(); int part = a.i(), sgprs_quantize_i8(d, x, y, sc, pool, part))
+METHOD(linear_i8, 12, auto* d = a.p<sgprs_linear_i8_desc_t>(); auto* x = a.p<int8_t>(); auto* sx = a.p<float>(); auto* w = a.p<int8_t>();
+       auto* sw = a.p<float>(); auto* bias = a.p<float>(); auto* res = a.p(); auto* y = a.p(); auto* ws = a.p(); size_t wb = a.z();
+       auto* pool = a.p<sgprs_pool_t>(); int part = a.i(), sgprs_linear_i8(d, x, sx, w, sw, bias, res, y, ws, wb, pool, part))
+METHOD(paged_append, 10, auto* d = a.p<sgprs_paged_append_desc_t>(); auto* k = a.p(); auto* v = a.p(); auto* off = a.p<int>(); auto* tab = a.p<int>();
+       auto* len = a.p<int>(); auto* kc = a.p(); auto* vc = a.p(); auto* pool = a.p<sgprs_pool_t>(); int part = a.i(),
+       sgprs_paged_append(d, k, v, off, tab, len, kc, vc, pool, part))
+METHOD(paged_attention, 11, auto* d = a.p<sgprs_paged_attention_desc_t>(); auto* q = a.p(); auto* kc = a.p(); auto* vc = a.p(); auto* tab = a.p<int>();
+       auto* len = a.p<int>(); auto* o = a.p(); auto* ws = a.p(); size_t wb = a.z(); auto* pool = a.p<sgprs_pool_t>(); int part = a.i(),
+       sgprs_paged_attention(d, q, kc, vc, tab, len, o, ws, wb, pool, part))
 METHOD(stage_run, 7, auto* t = a.p<sgprs_task_t>(); int st = a.i(); int b = a.i(); auto* in = a.p(); auto* out = a.p();
        auto* pool = a.p<sgprs_pool_t>(); int part = a.i(), sgprs_stage_run(t, st, b, in, out, pool, part))
 METHOD(task_run, 6, auto* t = a.p<sgprs_task_t>(); int b = a.i(); auto* in = a.p(); auto* lg = a.p<float>();
@@ -80,7 +94,8 @@ METHOD(task_run, 6, auto* t = a.p<sgprs_task_t>(); int b = a.i(); auto* in = a.p
 
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(conv2d), ENTRY(maxpool2d), ENTRY(bn_relu), ENTRY(add_relu), ENTRY(avgpool_fc), ENTRY(avgpool_fc_static),
-                         ENTRY(global_avgpool), ENTRY(linear), ENTRY(group_norm), ENTRY(attention), ENTRY(stage_run), ENTRY(task_run), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(global_avgpool), ENTRY(linear), ENTRY(group_norm), ENTRY(attention), ENTRY(rms_norm), ENTRY(quantize_i8),
+                         ENTRY(linear_i8), ENTRY(paged_append), ENTRY(paged_attention), ENTRY(stage_run), ENTRY(task_run), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "Hot entry points of libsgprs.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
