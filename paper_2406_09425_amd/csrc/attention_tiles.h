@@ -234,7 +234,8 @@ template <int DT, int HD> struct Running {
     __device__ __forceinline__ float total() const { return sum + other_half(sum); }
     // BLOCKS blocks of 32 keys from key0 on, in LDS at k_at and v_at; keys from first_unseen on are not seen.  k_done
     // is called when k has been read, v_ready before v is.
-    template <int BLOCKS, bool MASKED, class KDone, class VReady>
+    // ZEROS: v holds zeros at keys that are not seen, so that only the scores need a mask.
+    template <int BLOCKS, bool MASKED, bool ZEROS = false, class KDone, class VReady>
     __device__ __forceinline__ void tile(const u32x4_t* q, float scale_log2, unsigned k_at, unsigned v_at, int key0, int first_unseen, KDone k_done, VReady v_ready)
     {
         const unsigned k_base = place.hidden(place.k + k_at), v_base = place.hidden(place.v + v_at);
@@ -273,9 +274,9 @@ template <int DT, int HD> struct Running {
                 p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale_log2, -base));
                 sum += p[i];
             }
-            add_values<DT, HD, MASKED>(o, p, v_base, b, &odd);
+            add_values<DT, HD, MASKED && !ZEROS>(o, p, v_base, b, &odd);
         }
-        if constexpr (MASKED) {
+        if constexpr (MASKED && !ZEROS) {
             static_assert(BLOCKS == 1, "a block at a time");
             if (__any(odd)) add_not_finite<DT, HD>(o, v_base, 0, key0, first_unseen);
         }

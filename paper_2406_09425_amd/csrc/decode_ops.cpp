@@ -114,6 +114,8 @@ int check_paged_attention(const sgprs_paged_attention_desc_t* d, sgprs_paged_att
     if ((rc = check_cache(*d, full))) return rc;
     if (d->heads <= 0 || d->heads % d->kv_heads) return fail(SGPRS_ERR_INVALID_ARG, "%d heads are no positive multiple of %d key heads", d->heads, d->kv_heads);
     if (d->heads > 65535) return fail(SGPRS_ERR_UNSUPPORTED, "more than 65535 heads");
+    if ((long long)d->n_seqs * d->kv_heads * ((d->heads / d->kv_heads + 31) / 32) > (1 << 28))
+        return fail(SGPRS_ERR_UNSUPPORTED, "%d sequences of %d key heads: supported are up to 2^28 of both, and of 32 heads each", d->n_seqs, d->kv_heads);
     if (d->window < 0 || d->sinks < 0 || (d->sinks > 0 && d->window == 0))
         return fail(SGPRS_ERR_INVALID_ARG, "window %d, sinks %d: need both >= 0, and a window where there are sinks", d->window, d->sinks);
     if (!(d->scale > -3e38f && d->scale < 3e38f)) return fail(SGPRS_ERR_INVALID_ARG, "scale is not finite");

@@ -2,11 +2,12 @@
 //
 // Attention is bound by reading the cache.  The queries of all heads that share a key head are one block of 32 columns (or
 // several), so a key is read once for them.  An item is a sequence, a key head and a block; its visible positions, one
-// behind the other (first tokens, then the window), form units of 128.  Every workgroup finds the sum of all sequences'
-// units and takes an equal run of them, which may begin and end inside items: however different the lengths are, all
-// workgroups have the same to do.  An item that several of them share is joined by a second launch from partial sums, two
-// at most of a workgroup, in a fixed order.  Wavefront v of four takes every fourth tile of 32 keys of a run, k and v through
-// LDS buffers of its own, each row from wherever its page is: the table's entries come two tiles ahead of the loads.
+// behind the other (first tokens, then the window), form units of 128.  All items in a row are divided into runs of equal
+// cost, one for each workgroup, which may begin and end inside items: however different the lengths are, all workgroups
+// have the same to do.  An item that several of them share is joined by a second launch from partial sums, two at most of a
+// workgroup, in a fixed order.  Wavefront v of four takes every fourth tile of 32 keys of an item, k and v through LDS
+// buffers of its own, each row from wherever its page is.  Its requests run on over the end of an item: table entries come
+// two tiles ahead, the next item's first tile is on its way while this one's sums meet.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -17,7 +18,7 @@
 namespace sgprs {
 
 struct JoinRecord {
-    int seq, item, last, unused;  // what begins in a workgroup and ends in workgroup `last` (-1: nothing)
+    int seq, item, last, unused;  // what begins in a workgroup's run and ends in that of workgroup `last` (-1: nothing)
 };
 
 struct PagedArgs {
@@ -35,110 +36,167 @@ struct PagedArgs {
     long long hq, ho;                // bytes
     long long page_stride, token_stride, head_stride;  // bytes
     int row_blocks, rows;            // blocks of 32 heads of a key head; rows of the largest
-    float* part_o;                   // [workgroup][continued, begun][row][head_dim], weights relative to part_stat
-    float2* part_stat;               // [workgroup][continued, begun][row]: maximum, sum
+    int items;                       // of a sequence
+    unsigned heads_mul, grid_mul;
+    int heads_sh, grid_sh;           // item / kv_heads, cost / workgroups
+    int unit_log2;                   // tiles of a unit
+    float* part_o;                   // [workgroup][ended, not ended][row][head_dim], weights relative to part_stat
+    float2* part_stat;               // [workgroup][ended, not ended][row]: maximum, sum
     JoinRecord* records;             // [workgroup]
 };
 
-constexpr int kUnit = 128;           // positions: a tile of 32 for each wavefront
+constexpr int kWaves = 4;            // of a workgroup
 constexpr int kMaxWorkgroups = 2 * SGPRS_MAX_MASK_WORDS * 32;
+constexpr int kItemCost = 1;         // what an item costs beside its units, in units
+constexpr int kMeetRows = 4;         // rows whose sums meet in LDS at once
 
 __device__ __align__(16) unsigned paged_zeros[4] = {0, 0, 0, 0};  // what is loaded for positions behind the last
 
 __device__ __forceinline__ int quotient(int n, unsigned mul, int sh) { return (int)(__umulhi(2u * (unsigned)n, mul) >> sh); }
 
-__device__ __forceinline__ long long uniform(long long v)
-{
-#if __HIP_DEVICE_COMPILE__
-    return (long long)(unsigned)__builtin_amdgcn_readfirstlane((int)v) | (long long)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32;
-#else
-    return v;
-#endif
-}
-
 // The positions that a sequence's new token sees: n of them, the i-th at i or, from `sinks` on, at i + gap.
 struct Seen {
     int n, sinks, gap;
-    __device__ __forceinline__ int units() const { return max(1, (n + kUnit - 1) / kUnit); }  // (one to write zeros)
+    __device__ __forceinline__ int units(const PagedArgs& a) const { return max(1, (((n + 31) >> 5) + (1 << a.unit_log2) - 1) >> a.unit_log2); }  // (one to write zeros)
+    __device__ __forceinline__ int cost(const PagedArgs& a) const { return units(a) + kItemCost; }
 };
-__device__ __forceinline__ Seen seen_of(const PagedArgs& a, int seq)
+__device__ __forceinline__ Seen seen_of(const PagedArgs& a, int length)
 {
-    const int len = min(max(a.lens[seq], 0), a.table_width * a.page_size);
+    const int len = min(max(length, 0), a.table_width * a.page_size);
     const int first = a.window > 0 && len > a.window ? len - a.window : 0;
     const int sinks = min(a.sinks, first);
     return {sinks + len - first, sinks, first - sinks};
 }
 
-// Runs of an equal number of units (up to one): the first of workgroup w, and whose unit u is.
+__device__ __forceinline__ int kv_head_of(const PagedArgs& a, int item) { return item - quotient(item, a.heads_mul, a.heads_sh) * a.kv_heads; }
+
+// Runs of an equal cost (up to one): the first unit of workgroup w's, and whose a unit is.
 struct Runs {
-    long long per, rest;
-    __device__ __forceinline__ Runs(long long units, int workgroups) : per(units / workgroups), rest(units % workgroups) {}
-    __device__ __forceinline__ long long first(int w) const { return w * per + min((long long)w, rest); }
-    __device__ __forceinline__ int owner(long long u) const { return (int)(u < rest * (per + 1) ? u / (per + 1) : rest + (u - rest * (per + 1)) / per); }
+    int per, rest;
+    __device__ __forceinline__ Runs(const PagedArgs& a, int cost, int runs) : per(quotient(cost, a.grid_mul, a.grid_sh)), rest(cost - per * runs) {}
+    __device__ __forceinline__ int first(int w) const { return w * per + min(w, rest); }
+    __device__ __forceinline__ int owner(int u) const
+    {
+        const unsigned longer = rest * (per + 1u);
+        return (unsigned)u < longer ? (unsigned)u / (per + 1u) : rest + ((unsigned)u - longer) / (unsigned)per;
+    }
 };
 
 template <int DT, int HD> struct PagedShape {
     static constexpr int HALF = 32 * KvTile<DT, HD>::ROW, STAGE = 2 * HALF;  // k, and v behind it
-    static constexpr int NW = 4;
     static constexpr int SROW = HD + 4;                                       // floats of a row where the sums meet
-    static constexpr int JOIN = NW * (32 * SROW + 64) * 4, LDS = NW * STAGE > JOIN ? NW * STAGE : JOIN;
-    static constexpr int PER_CU = LDS > 81856 ? 1 : 2;
+    static constexpr int MEET = kWaves * STAGE, LDS = MEET + kWaves * kMeetRows * (SROW + 2) * 4;
+    static constexpr int PER_CU = LDS > 81920 ? 1 : 2;
 };
+
+#if __HIP_DEVICE_COMPILE__
+// What a run has of an item, the same for all lanes.
+struct Segment {
+    int seq, item, n, sinks, gap;  // item: of the sequence; n: positions
+    int first, end, tiles;         // tiles that it has, of so many
+    __device__ __forceinline__ bool begins() const { return first == 0; }
+    __device__ __forceinline__ bool ends() const { return end == tiles; }
+};
+#endif
 
 template <int DT, int HD> __global__ __launch_bounds__(256, (PagedShape<DT, HD>::PER_CU)) void paged_attention_kernel(const PagedArgs a)
 {
 #if __HIP_DEVICE_COMPILE__
     typedef KvTile<DT, HD> Tile;
     typedef PagedShape<DT, HD> Shape;
-    constexpr int ES = Tile::ES, STEPS = HD * ES / 32, NW = Shape::NW, LOADS = Shape::HALF / 1024, RPI = 1024 / Tile::ROW;
+    constexpr int ES = Tile::ES, STEPS = HD * ES / 32, NW = kWaves, LOADS = Shape::HALF / 1024, RPI = 1024 / Tile::ROW;
     extern __shared__ __align__(16) unsigned char smem[];  // (all of the LDS, from address 0 on)
-    long long* totals = (long long*)(smem + Shape::LDS);
-    long long& found_start = totals[4];
-    int& found_seq = *(int*)(totals + 5);
+    int* scratch = (int*)(smem + Shape::MEET);
     const int lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int heads_and_blocks = a.kv_heads * a.row_blocks;
 
-    // ---- this workgroup's run of units, and the sequence it begins in ----
-    const int share = (a.n_seqs + 255) >> 8, s0 = min((int)threadIdx.x * share, a.n_seqs), s1 = min(s0 + share, a.n_seqs);
-    long long mine = 0;
-    for (int s = s0; s < s1; ++s) mine += seen_of(a, s).units();
-    long long upto = mine;
+    // ---- this workgroup's run, and the sequence that it begins in ----
+    int seq, start, length, cost;  // start: the cost of the sequences before it
+    if (a.n_seqs <= 64) {
+        length = lane < a.n_seqs ? a.lens[lane] : 0;
+        const int mine = lane < a.n_seqs ? seen_of(a, length).cost(a) * a.items : 0;
+        int upto = mine;
 #pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-        const long long left = __shfl_up(upto, x);
-        if (lane >= x) upto += left;
-    }
-    if (lane == 63) totals[wave] = upto;
-    if (threadIdx.x == 0) found_seq = a.n_seqs;
-    __syncthreads();
-    long long units = 0;
-#pragma unroll
-    for (int v = 0; v < NW; ++v) {
-        if (v == wave) upto += units;
-        units += totals[v];
-    }
-    const Runs runs(units * heads_and_blocks, gridDim.x);
-    const long long run_begin = uniform(runs.first(blockIdx.x)), run_end = uniform(runs.first(blockIdx.x + 1));
-    if (threadIdx.x == 0) a.records[blockIdx.x] = {0, 0, -1, 0};
-    if (run_begin >= run_end) return;
-    if ((upto - mine) * heads_and_blocks <= run_begin && run_begin < upto * heads_and_blocks) {
-        long long start = upto - mine;
-        int s = s0;
-        for (; s + 1 < s1; ++s) {
-            const int n = seen_of(a, s).units();
-            if (run_begin < (start + n) * heads_and_blocks) break;
-            start += n;
+        for (int x = 1; x < 64; x <<= 1) {
+            const int left = __shfl_up(upto, x);
+            if (lane >= x) upto += left;
         }
-        found_seq = s;
-        found_start = start * heads_and_blocks;
+        cost = __builtin_amdgcn_readlane(upto, 63);
+        const int begin = Runs(a, cost, gridDim.x).first(blockIdx.x);
+        seq = min((int)__popcll(__ballot(upto <= begin)), a.n_seqs - 1);  // (the costs rise, and those behind the last one are its)
+        start = __builtin_amdgcn_readlane(upto - mine, seq);
+        length = __builtin_amdgcn_readlane(length, seq);
+    } else {
+        const int share = (a.n_seqs + 255) >> 8, s0 = min((int)threadIdx.x * share, a.n_seqs), s1 = min(s0 + share, a.n_seqs);
+        int mine = 0;
+        for (int s = s0; s < s1; ++s) mine += seen_of(a, a.lens[s]).cost(a) * a.items;
+        int upto = mine;
+#pragma unroll
+        for (int x = 1; x < 64; x <<= 1) {
+            const int left = __shfl_up(upto, x);
+            if (lane >= x) upto += left;
+        }
+        if (lane == 63) scratch[wave] = upto;
+        if (threadIdx.x == 0) scratch[NW] = a.n_seqs;
+        __syncthreads();
+        cost = 0;
+#pragma unroll
+        for (int v = 0; v < NW; ++v) {
+            if (v == wave) upto += cost;
+            cost += scratch[v];
+        }
+        const int begin = Runs(a, cost, gridDim.x).first(blockIdx.x);
+        if (upto - mine <= begin && begin < upto) {
+            int s = s0, before = upto - mine;
+            for (; s < s1; ++s) {
+                length = a.lens[s];
+                const int c = seen_of(a, length).cost(a) * a.items;
+                if (begin < before + c) break;
+                before += c;
+            }
+            scratch[NW] = s;
+            scratch[NW + 1] = before;
+            scratch[NW + 2] = length;
+        }
+        __syncthreads();
+        cost = __builtin_amdgcn_readfirstlane(cost);
+        seq = __builtin_amdgcn_readfirstlane(scratch[NW]);
+        start = __builtin_amdgcn_readfirstlane(scratch[NW + 1]);
+        length = __builtin_amdgcn_readfirstlane(scratch[NW + 2]);
+        __syncthreads();
     }
-    __syncthreads();
+    const Runs runs(a, cost, gridDim.x);
+    int at = runs.first(blockIdx.x);
+    const int run_end = runs.first(blockIdx.x + 1);
+    if (threadIdx.x == 0) a.records[blockIdx.x] = {0, 0, -1, 0};
+    if (at >= run_end || seq >= a.n_seqs) return;
+
+    Seen seen = seen_of(a, length);
+    int item_cost = seen.cost(a), item = (int)((unsigned)(at - start) / (unsigned)item_cost), offset = at - start - item * item_cost;
+    // The next item of the run that has tiles in it; false at the run's end.
+    auto next_segment = [&](Segment& s) {
+        while (at < run_end) {
+            if (item == a.items) {
+                item = 0;
+                if (++seq >= a.n_seqs) return false;
+                seen = seen_of(a, a.lens[seq]);
+                item_cost = seen.cost(a);
+            }
+            const int here = min(run_end - at, item_cost - offset), tiles = max(1, (seen.n + 31) >> 5);
+            const int first = max(offset - kItemCost, 0) << a.unit_log2, end = min(max(offset + here - kItemCost, 0) << a.unit_log2, tiles);
+            s = {seq, item, seen.n, seen.sinks, seen.gap, first, end, tiles};
+            at += here;
+            offset = 0;
+            ++item;
+            if (first < end) return true;
+        }
+        return false;
+    };
 
     const int row_bytes = a.head_dim * ES;
     const int lrow = lane / Tile::CHUNKS, slot = (lane % Tile::CHUNKS) ^ Tile::swizzle(lrow);
     unsigned char* buffers = smem + wave * Shape::STAGE;
-    const unsigned at = (unsigned)(wave * Shape::STAGE);
+    const unsigned buffers_at = (unsigned)(wave * Shape::STAGE);
     auto landed = [](auto behind) {  // all but the last `behind` requests
         constexpr int N = decltype(behind)::value;
         __builtin_amdgcn_sched_barrier(0);
@@ -150,129 +208,148 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (PagedShape<DT, HD>:
         __builtin_amdgcn_s_waitcnt(0xC07F);
         __builtin_amdgcn_sched_barrier(0);
     };
-
-    int seq = __builtin_amdgcn_readfirstlane(found_seq);
-    long long seq_start = uniform(found_start), unit = run_begin;
-    while (unit < run_end && seq < a.n_seqs) {
-        const Seen seen = seen_of(a, seq);
-        const int n_units = seen.units();
-        if (unit - seq_start >= (long long)n_units * heads_and_blocks) {
-            seq_start += (long long)n_units * heads_and_blocks;
-            ++seq;
-            continue;
-        }
-        const int item = (int)((unit - seq_start) / n_units), unit0 = (int)(unit - seq_start - (long long)item * n_units);
-        const int take = (int)min(run_end - unit, (long long)(n_units - unit0));
-        const int kv_head = item % a.kv_heads, block = item / a.kv_heads;
-        const int rows = min(32, a.group - block * 32);
-        const int first_head = kv_head * a.group + block * 32, head = first_head + min(col, rows - 1);
-        const int begin = unit0 * kUnit, end = min(seen.n, (unit0 + take) * kUnit);
-        const int tiles = (end - begin + 31) >> 5;
-        const int* table = a.table + (long long)seq * a.table_width;
-        const unsigned char* kp = a.k + kv_head * a.head_stride;
-        const unsigned char* vp = a.v + kv_head * a.head_stride;
-
-        // lane l looks after key l of a tile: its page first, then its place
-        auto position = [&](int t) {
-            const int i = min(begin + t * 32 + col, end - 1);
-            return i < seen.sinks ? i : i + seen.gap;
-        };
-        auto entry_of = [&](int t) { return table[quotient(position(t), a.page_mul, a.page_sh)]; };
-        auto place_of = [&](int t, int entry) {  // -1 behind the last key
-            const int p = position(t), page = min((unsigned)entry, (unsigned)a.n_pages - 1u);
-            const int in = p - quotient(p, a.page_mul, a.page_sh) * a.page_size;
-            return begin + t * 32 + col < end ? page * a.page_stride + in * a.token_stride : -1;
-        };
-        auto request = [&](const unsigned char* from, unsigned char* to, long long place) {
-            int lane_row = lrow;
-            asm volatile("" : "+v"(lane_row));  // what follows from it is worked out in every tile rather than kept in registers
+    // lane l looks after key l of a tile: its page first, then its place (-1 behind the segment's last key)
+    auto position = [&](const Segment& s, int t) {
+        const int i = max(min(t * 32 + col, s.n - 1), 0);
+        return i < s.sinks ? i : i + s.gap;
+    };
+    auto entry_of = [&](const Segment& s, int t) {
+        return s.n > 0 ? a.table[(long long)s.seq * a.table_width + quotient(position(s, t), a.page_mul, a.page_sh)] : 0;
+    };
+    auto place_of = [&](const Segment& s, int t, int entry) {
+        const int p = position(s, t), page = min((unsigned)entry, (unsigned)a.n_pages - 1u);
+        const int in = p - quotient(p, a.page_mul, a.page_sh) * a.page_size;
+        const long long place = page * a.page_stride + in * a.token_stride + kv_head_of(a, s.item) * a.head_stride;
+        return t < s.end && t * 32 + col < s.n ? place : -1;
+    };
+    auto request = [&](const unsigned char* cache, unsigned char* to, long long place) {
+        int lane_row = lrow;
+        asm volatile("" : "+v"(lane_row));  // what follows from it is worked out in every tile rather than kept in registers
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int chunk = (slot ^ Tile::swizzle(i * RPI)) << 4;
-                const long long at = __shfl(place, i * RPI + lane_row);
-                const unsigned char* p = at >= 0 && chunk < row_bytes ? from + at + chunk : (const unsigned char*)paged_zeros;
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (lds_ptr_t)(to + i * 1024), 16, 0, 0);
-            }
-        };
+        for (int i = 0; i < LOADS; ++i) {
+            const int chunk = (slot ^ Tile::swizzle(i * RPI)) << 4;
+            const long long row = __shfl(place, i * RPI + lane_row);
+            const unsigned char* p = row >= 0 && chunk < row_bytes ? cache + row + chunk : (const unsigned char*)paged_zeros;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (lds_ptr_t)(to + i * 1024), 16, 0, 0);
+        }
+    };
+    u32x4_t q[STEPS];
+    auto load_q = [&](const Segment& s) {
+        const int kv_head = kv_head_of(a, s.item), block = quotient(s.item, a.heads_mul, a.heads_sh);
+        const unsigned char* qp = a.q + (long long)s.seq * a.ldq + (kv_head * a.group + min(block * 32 + col, a.group - 1)) * a.hq;
+#pragma unroll
+        for (int c = 0; c < STEPS; ++c) q[c] = (2 * c + h) * 16 < row_bytes ? *(const u32x4_t*)(qp + (2 * c + h) * 16) : u32x4_t{0, 0, 0, 0};
+    };
 
+    Segment now = {}, next = {};
+    if (!next_segment(now)) return;
+    int t = now.first + wave;
+    const int first_entry = entry_of(now, t);
+    int entry = entry_of(now, t + NW), next_entry = 0;
+    load_q(now);
+    long long place = place_of(now, t, first_entry);
+    __builtin_amdgcn_sched_barrier(0);
+    request(a.k, buffers, place);
+    request(a.v, buffers + Shape::HALF, place);
+    for (;;) {
+        const bool more = next_segment(next);
+        const int next_t = next.first + wave;
+        int next_place_entry = 0;
+        if (more) {
+            next_place_entry = entry_of(next, next_t);
+            next_entry = entry_of(next, next_t + NW);
+        }
+#pragma unroll
+        for (int c = 0; c < STEPS; ++c) q[c] ^= a.q_flip;
         Running<DT, HD> run;
         run.start();
-        if (tiles > 0) {
-            u32x4_t q[STEPS];
-            const unsigned char* qp = a.q + (long long)seq * a.ldq + head * a.hq;
-#pragma unroll
-            for (int c = 0; c < STEPS; ++c) {
-                q[c] = (2 * c + h) * 16 < row_bytes ? *(const u32x4_t*)(qp + (2 * c + h) * 16) : u32x4_t{0, 0, 0, 0};
-                q[c] ^= a.q_flip;
-            }
-            long long place = place_of(wave, entry_of(wave));
-            int entry = entry_of(wave + NW);
-            request(kp, buffers, place);
-            request(vp, buffers + Shape::HALF, place);
-            for (int t = wave; t < tiles; t += NW) {
-                landed(std::integral_constant<int, LOADS>());  // k, before v
-                const int key0 = begin + t * 32;
-                auto k_done = [&] {
-                    read();
-                    place = place_of(t + NW, entry);
-                    entry = entry_of(t + 2 * NW);
-                    __builtin_amdgcn_sched_barrier(0);
-                    request(kp, buffers, place);
-                };
-                auto v_ready = [&] { landed(std::integral_constant<int, LOADS + 1>()); };  // v, before an entry and the next k
-                if (key0 + 32 <= end) run.template tile<1, false>(q, a.scale_log2, at, at + Shape::HALF, key0, end, k_done, v_ready);
-                else run.template tile<1, true>(q, a.scale_log2, at, at + Shape::HALF, key0, end, k_done, v_ready);
+        // a tile for each wavefront at least, if only one without keys
+        do {
+            landed(std::integral_constant<int, LOADS>());  // k, before v
+            auto k_done = [&] {
                 read();
-                request(vp, buffers + Shape::HALF, place);
-            }
-            __builtin_amdgcn_s_waitcnt(0);  // requests past the end bring zeros
-        }
-        __syncthreads();
-        float* sums = (float*)smem;  // [wavefront][column][channel], then [wavefront][column] maxima and sums
-        float* tops = sums + NW * 32 * Shape::SROW;
-        float* sum_of = tops + NW * 32;
-        if (col < rows) {
-#pragma unroll
-            for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4)
-                    *(float4*)(sums + (wave * 32 + col) * Shape::SROW + d * 32 + (i >> 2) * 8 + h * 4) = make_float4(run.o[d][i], run.o[d][i + 1], run.o[d][i + 2], run.o[d][i + 3]);
-        }
+                if (t + NW < now.end) {
+                    place = place_of(now, t + NW, entry);
+                    entry = entry_of(now, t + 2 * NW);
+                } else {
+                    place = more ? place_of(next, next_t, next_place_entry) : -1;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                request(a.k, buffers, place);
+            };
+            auto v_ready = [&] { landed(std::integral_constant<int, LOADS>()); };  // v, before the next k
+            run.template tile<1, true, true>(q, a.scale_log2, buffers_at, buffers_at + Shape::HALF, t * 32, min(now.n, now.end * 32), k_done, v_ready);
+            read();
+            request(a.v, buffers + Shape::HALF, place);
+            t += NW;
+        } while (t < now.end);
+        if (more) load_q(next);
+
+        // ---- the wavefronts' sums meet ----
+        const int kv_head = kv_head_of(a, now.item), block = quotient(now.item, a.heads_mul, a.heads_sh);
+        const int rows = min(32, a.group - block * 32), first_head = kv_head * a.group + block * 32, vecs = a.head_dim >> 2;
+        const bool whole = now.begins() && now.ends();
+        const long long part = ((long long)blockIdx.x * 2 + !now.ends()) * a.rows;
         const float sum = run.total();
-        if (h == 0) {
-            tops[wave * 32 + col] = run.top;
-            sum_of[wave * 32 + col] = sum;
-        }
-        __syncthreads();
-        const int vecs = a.head_dim >> 2;
-        const bool whole = take == n_units;
-        const long long part = ((long long)blockIdx.x * 2 + (unit0 == 0)) * a.rows;
-        for (int e = threadIdx.x; e < rows * vecs; e += NW * 64) {
-            const int r = e / vecs, c = (e - r * vecs) * 4;
-            float top = tops[r], total = 0.f, z[4] = {};
+        float* sums = (float*)(smem + Shape::MEET);  // [wavefront][row][channel], then [wavefront][row] maxima and sums
+        float* tops = sums + NW * kMeetRows * Shape::SROW;
+        float* sum_of = tops + NW * kMeetRows;
+        auto meet = [] {  // (without waiting for what is on its way from memory)
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0xC07F);
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        for (int r0 = 0; r0 < rows; r0 += kMeetRows) {
+            meet();
+            if (col >= r0 && col < r0 + kMeetRows) {
+                const int r = wave * kMeetRows + col - r0;
 #pragma unroll
-            for (int v = 1; v < NW; ++v) top = fmaxf(top, tops[v * 32 + r]);
+                for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
-            for (int v = 0; v < NW; ++v) {
-                const float t = tops[v * 32 + r], w = t == top ? 1.f : __builtin_amdgcn_exp2f(t - top);  // (both may be -inf: sums of 0)
-                total = __builtin_fmaf(sum_of[v * 32 + r], w, total);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) z[x] = __builtin_fmaf(sums[(v * 32 + r) * Shape::SROW + c + x], w, z[x]);
+                    for (int i = 0; i < 16; i += 4)
+                        *(float4*)(sums + r * Shape::SROW + d * 32 + (i >> 2) * 8 + h * 4) = make_float4(run.o[d][i], run.o[d][i + 1], run.o[d][i + 2], run.o[d][i + 3]);
+                tops[r] = run.top;
+                sum_of[r] = sum;
             }
-            if (whole) {
-                const float inv = normaliser(total, seen.n > 0);
+            meet();
+            for (int e = threadIdx.x; e < min(kMeetRows, rows - r0) * 32; e += NW * 64) {
+                const int r = e >> 5, c = (e & 31) * 4;
+                if (c >= a.head_dim) continue;
+                float top = tops[r], total = 0.f, z[4] = {};
 #pragma unroll
-                for (int x = 0; x < 4; ++x) z[x] *= inv;
-                store4<DT>(a.o + (long long)seq * a.ldo + (first_head + r) * a.ho, c, z);
-            } else {
-                *(float4*)(a.part_o + (part + r) * a.head_dim + c) = make_float4(z[0], z[1], z[2], z[3]);
-                if (c == 0) a.part_stat[part + r] = make_float2(top, total);
+                for (int v = 1; v < NW; ++v) top = fmaxf(top, tops[v * kMeetRows + r]);
+#pragma unroll
+                for (int v = 0; v < NW; ++v) {
+                    const float m = tops[v * kMeetRows + r], w = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);  // (both may be -inf: sums of 0)
+                    total = __builtin_fmaf(sum_of[v * kMeetRows + r], w, total);
+                    const float4 o = *(const float4*)(sums + (v * kMeetRows + r) * Shape::SROW + c);
+                    z[0] = __builtin_fmaf(o.x, w, z[0]);
+                    z[1] = __builtin_fmaf(o.y, w, z[1]);
+                    z[2] = __builtin_fmaf(o.z, w, z[2]);
+                    z[3] = __builtin_fmaf(o.w, w, z[3]);
+                }
+                if (whole) {
+                    const float inv = normaliser(total, now.n > 0);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) z[x] *= inv;
+                    store4<DT>(a.o + (long long)now.seq * a.ldo + (first_head + r0 + r) * a.ho, c, z);
+                } else {
+                    *(float4*)(a.part_o + (part + r0 + r) * a.head_dim + c) = make_float4(z[0], z[1], z[2], z[3]);
+                    if (c == 0) a.part_stat[part + r0 + r] = make_float2(top, total);
+                }
             }
         }
-        if (!whole && unit0 == 0 && threadIdx.x == 0) a.records[blockIdx.x] = {seq, item, runs.owner(unit + n_units - 1), 0};
-        unit += take;
-        __syncthreads();  // the buffers are free again
+        if (now.begins() && !now.ends() && threadIdx.x == 0) {
+            const int units = (now.tiles + (1 << a.unit_log2) - 1) >> a.unit_log2;  // the run's end is behind unit end of them
+            a.records[blockIdx.x] = {now.seq, now.item, min(runs.owner(run_end + units - (now.end >> a.unit_log2) - 1), (int)gridDim.x - 1), 0};
+        }
+        if (!more) break;
+        now = next;
+        t = next_t;
+        entry = next_entry;
     }
+    __builtin_amdgcn_s_waitcnt(0);  // the last requests bring zeros
 #endif
 }
 
@@ -287,10 +364,10 @@ template <int DT> __global__ __launch_bounds__(256) void paged_join_kernel(const
     const JoinRecord record = a.records[blockIdx.x];
     if (record.last < 0) return;
     const int n = record.last - (int)blockIdx.x + 1;
-    const int kv_head = record.item % a.kv_heads, block = record.item / a.kv_heads, rows = min(32, a.group - block * 32);
+    const int kv_head = kv_head_of(a, record.item), block = quotient(record.item, a.heads_mul, a.heads_sh), rows = min(32, a.group - block * 32);
     const int tid = threadIdx.x, lane = tid & 31, group = tid >> 5, c = lane * 4;
     for (int r = blockIdx.y; r < rows; r += gridDim.y) {
-        auto part = [&](int p) { return ((long long)(blockIdx.x + p) * 2 + (p == 0)) * a.rows + r; };
+        auto part = [&](int p) { return ((long long)(blockIdx.x + p) * 2 + (p != n - 1)) * a.rows + r; };
         float top = -INFINITY, total = 0.f;
         for (int p = tid; p < n; p += 256) top = fmaxf(top, a.part_stat[part(p)].x);
 #pragma unroll
@@ -392,7 +469,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs a)
 
 // ---- plans -------------------------------------------------------------------------------------
 struct PagedPlan {
-    int workgroups, row_blocks, rows;
+    int workgroups, row_blocks, rows, unit_log2;
     bool join;
 };
 
@@ -404,19 +481,22 @@ static PagedPlan plan_paged(const sgprs_paged_attention_desc_t& d, int cus)
     p.rows = std::min(32, group);
     long long most = (long long)d.table_width * d.page_size;  // positions that a token can see
     if (d.window > 0) most = std::min(most, (long long)d.window + d.sinks);
-    const long long units = (most + kUnit - 1) / kUnit, items = (long long)d.n_seqs * d.kv_heads * p.row_blocks;
+    const long long tiles = std::max(1ll, (most + 31) / 32), items = (long long)d.n_seqs * d.kv_heads * p.row_blocks;
+    p.unit_log2 = 2;  // a tile for each wavefront; more where the cost of all items could pass 2^31
+    while (items * (((tiles - 1) >> p.unit_log2) + 1 + kItemCost) >= (1ll << 31)) ++p.unit_log2;
+    const long long units = ((tiles - 1) >> p.unit_log2) + 1;
     const bool wide = d.dtype == SGPRS_F32 && d.head_dim > 64;
-    p.workgroups = (int)std::min<long long>(std::min(kMaxWorkgroups, (wide ? 1 : 2) * cus), (double)units * items > 1e6 ? 1000000 : units * items);
+    p.workgroups = (int)std::min<long long>(std::min(kMaxWorkgroups, (wide ? 1 : 2) * cus), items * (units + kItemCost));
     p.join = units > 1;
     return p;
 }
 
-static size_t part_floats(const sgprs_paged_attention_desc_t& d, const PagedPlan& p) { return (size_t)p.workgroups * 2 * p.rows * d.head_dim; }
+static size_t part_rows(const PagedPlan& p) { return (size_t)p.workgroups * 2 * p.rows; }
 
 size_t paged_attention_workspace_bytes(const sgprs_paged_attention_desc_t& d, int cus)
 {
     const PagedPlan p = plan_paged(d, cus);
-    return p.workgroups * sizeof(JoinRecord) + part_floats(d, p) * 4 + (size_t)p.workgroups * 2 * p.rows * sizeof(float2);
+    return p.workgroups * sizeof(JoinRecord) + part_rows(p) * (d.head_dim * sizeof(float) + sizeof(float2));
 }
 
 template <auto kernel> static int launch_sized(dim3 grid, int lds, const PagedArgs& a, hipStream_t stream)
@@ -435,10 +515,10 @@ template <int DT> static int launch_typed(const PagedArgs& a, const PagedPlan& p
 {
     const dim3 grid((unsigned)p.workgroups);
     int rc;
-    if (a.head_dim <= 32) rc = launch_sized<paged_attention_kernel<DT, 32>>(grid, PagedShape<DT, 32>::LDS + 64, a, stream);
-    else if (a.head_dim <= 64) rc = launch_sized<paged_attention_kernel<DT, 64>>(grid, PagedShape<DT, 64>::LDS + 64, a, stream);
-    else if (a.head_dim <= 96) rc = launch_sized<paged_attention_kernel<DT, 96>>(grid, PagedShape<DT, 96>::LDS + 64, a, stream);
-    else rc = launch_sized<paged_attention_kernel<DT, 128>>(grid, PagedShape<DT, 128>::LDS + 64, a, stream);
+    if (a.head_dim <= 32) rc = launch_sized<paged_attention_kernel<DT, 32>>(grid, PagedShape<DT, 32>::LDS, a, stream);
+    else if (a.head_dim <= 64) rc = launch_sized<paged_attention_kernel<DT, 64>>(grid, PagedShape<DT, 64>::LDS, a, stream);
+    else if (a.head_dim <= 96) rc = launch_sized<paged_attention_kernel<DT, 96>>(grid, PagedShape<DT, 96>::LDS, a, stream);
+    else rc = launch_sized<paged_attention_kernel<DT, 128>>(grid, PagedShape<DT, 128>::LDS, a, stream);
     if (rc || !p.join) return rc;
     return launch_sized<paged_join_kernel<DT>>(dim3((unsigned)p.workgroups, (unsigned)std::min(p.rows, 8)), 0, a, stream);
 }
@@ -477,9 +557,13 @@ int launch_paged_attention(const sgprs_paged_attention_desc_t& d, const void* q,
     a.head_stride = d.head_stride * es;
     a.row_blocks = p.row_blocks;
     a.rows = p.rows;
+    a.items = d.kv_heads * p.row_blocks;
+    div_constants(d.kv_heads, &a.heads_mul, &a.heads_sh);
+    div_constants(p.workgroups, &a.grid_mul, &a.grid_sh);
+    a.unit_log2 = p.unit_log2;
     a.records = (JoinRecord*)ws;
     a.part_o = (float*)(a.records + p.workgroups);
-    a.part_stat = (float2*)(a.part_o + part_floats(d, p));
+    a.part_stat = (float2*)(a.part_o + part_rows(p) * d.head_dim);
     return d.dtype == SGPRS_BF16 ? launch_typed<SGPRS_BF16>(a, p, stream) : launch_typed<SGPRS_F32>(a, p, stream);
 }
 
