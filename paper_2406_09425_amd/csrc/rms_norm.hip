@@ -1,9 +1,11 @@
 // Root-mean-square norm of rows with the residual's addition, and rows of 8-bit integers with a scale each.
 //
-// A row is read once and kept in the registers of a wavefront or a workgroup (rows beyond that are read twice).  The sum of
-// squares and the largest value are held in 64 bits, where no square of a 32-bit number overflows or vanishes.
-// With t = h gamma a row's integers are 127 t / max|t|: the norm's factor cancels, so they need no statistics but the
-// maximum, and in 64 bits t is exact, so that they are those of the definition whatever the order of anything.
+// Bound by the memory.  A row is read once and kept in the registers of a wavefront or a workgroup (rows beyond that are
+// read twice).  With t = h gamma a row's integers are 127 t / max|t|: the norm's factor cancels, so they need no
+// statistics but the maximum, and they are to be those of the definition whatever the order of anything.  So they are
+// worked out in 32 bits, which leaves a quotient off by less than 2^-15, and those within 2^-15 of a border between two
+// integers are decided in 64 bits, in which t is exact.  Rows whose squares or products could leave the range of
+// 32-bit numbers, and rows that are not finite, go through 64 bits altogether.
 #include <algorithm>
 
 #include "decode_ops.h"
@@ -70,12 +72,15 @@ template <int DT> struct RowVec {
         }
         return v;
     }
-    static __device__ __forceinline__ void store_i8(unsigned char* p, const int* q, int live)
+    // q: integers in the low bytes
+    static __device__ __forceinline__ void store_i8(unsigned char* p, const unsigned* q, int live)
     {
         unsigned w[V / 4];
+#if __HIP_DEVICE_COMPILE__
 #pragma unroll
         for (int d = 0; d < V / 4; ++d)
-            w[d] = (q[4 * d] & 255u) | (q[4 * d + 1] & 255u) << 8 | (q[4 * d + 2] & 255u) << 16 | (unsigned)q[4 * d + 3] << 24;
+            w[d] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[4 * d + 3], q[4 * d + 2], 0x0c0c0400u), __builtin_amdgcn_perm(q[4 * d + 1], q[4 * d], 0x0c0c0400u), 0x05040100u);
+#endif
         if (live >= V) {
             __builtin_memcpy(p, w, V);
         } else {
@@ -84,35 +89,43 @@ template <int DT> struct RowVec {
                 if (e < live) p[e] = (unsigned char)(w[e / 4] >> (e % 4 * 8));
         }
     }
+    // V factors from channel c on, of which `live` exist
+    static __device__ __forceinline__ void load_factors(const float* p, int live, float* g)
+    {
+        if (live >= V) {
+            __builtin_memcpy(g, p, V * 4);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) g[e] = e < live ? p[e] : 1.f;
+        }
+    }
 };
 
-// What a row comes to, joined over its THREADS threads in a fixed order.
-struct RowStat {
-    double squares, most;
-    int odd;  // an infinity or a NaN among the t
+// Sums and maxima over a row's threads, in a fixed order.
+template <int THREADS> struct RowJoin {
+    double squares[THREADS / 64], most[THREADS / 64];
+    unsigned bits[THREADS / 64];
 };
-template <int THREADS> __device__ __forceinline__ RowStat join(RowStat s, RowStat* shared)
+struct Add {
+    template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return a + b; }
+};
+struct Most {
+    template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return a > b ? a : b; }
+};
+template <class Op, class T> __device__ __forceinline__ T over_wavefront(T v, Op op)
 {
 #if __HIP_DEVICE_COMPILE__
 #pragma unroll
-    for (int x = 32; x; x >>= 1) {
-        s.squares += __shfl_xor(s.squares, x);
-        s.most = fmax(s.most, __shfl_xor(s.most, x));
-    }
-    s.odd = __any(s.odd);
-    if constexpr (THREADS > 64) {
-        if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = s;
-        __syncthreads();
-        s = shared[0];
-#pragma unroll
-        for (int w = 1; w < THREADS / 64; ++w) {
-            s.squares += shared[w].squares;
-            s.most = fmax(s.most, shared[w].most);
-            s.odd |= shared[w].odd;
-        }
-    }
+    for (int x = 32; x; x >>= 1) v = op(v, __shfl_xor(v, x));
 #endif
-    return s;
+    return v;
+}
+template <int WAVES, class Op, class T> __device__ __forceinline__ T over_wavefronts(const T* all, Op op)
+{
+    T v = all[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v = op(v, all[w]);
+    return v;
 }
 
 // THREADS threads a row (a wavefront: four rows a workgroup), VPT vectors of it each; VPT 0: as many as it takes, read twice.
@@ -120,101 +133,255 @@ template <int DT, int KIND, int THREADS, int VPT> __global__ __launch_bounds__(T
 {
 #if __HIP_DEVICE_COMPILE__
     typedef RowVec<DT> Vec;
-    constexpr int V = Vec::V, ES = Vec::ES;
-    __shared__ RowStat shared[THREADS / 64];
-    const int thread = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
+    constexpr int V = Vec::V, WAVES = THREADS / 64;
+    __shared__ RowJoin<THREADS> joined;
+    const int thread = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x, wave = THREADS == 64 ? 0 : threadIdx.x >> 6;
     const int row = THREADS == 64 ? blockIdx.x * 4 + (int)(threadIdx.x >> 6) : blockIdx.x;
     if (row >= a.m) return;
     const unsigned char* xp = a.x + row * a.ldx;
     const unsigned char* rp = KIND != kQuantize && a.residual ? a.residual + row * a.ldr : nullptr;
     unsigned char* hp = KIND != kQuantize && a.sum ? a.sum + row * a.ldh : nullptr;
     unsigned char* yp = a.y + row * a.ldy;
+    const float* gamma = KIND != kQuantize ? a.gamma : nullptr;
     const int vectors = (a.c + V - 1) / V;
 
-    auto stream = [&](int v) {  // h
-        const int live = a.c - v * V;
-        u32x4_t h = Vec::load(xp + (long long)v * 16, live);
-        if (rp) {
-            const u32x4_t r = Vec::load(rp + (long long)v * 16, live);
-            float z[V];
+    auto added = [&](u32x4_t x, u32x4_t r) {
+        float z[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) z[e] = Vec::get(h, e) + Vec::get(r, e);
-            h = Vec::pack(z);
-        }
-        return h;
+        for (int e = 0; e < V; ++e) z[e] = Vec::get(x, e) + Vec::get(r, e);
+        return Vec::pack(z);
     };
     auto load_gamma = [&](int v, float* g) {
+        if (gamma) {
+            Vec::load_factors(gamma + v * V, a.c - v * V, g);
+        } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e) g[e] = KIND != kQuantize && a.gamma && v * V + e < a.c ? a.gamma[v * V + e] : 1.f;
+            for (int e = 0; e < V; ++e) g[e] = 1.f;
+        }
     };
-    RowStat stat = {0.0, 0.0, 0};
+    auto in_64_bits = [&](float h, float g) { return KIND == kQuantize ? (double)h : (double)h * (double)g; };
+    auto integer = [&](double t, double most) { return (unsigned)(int)rint(127.0 * t / most); };
+
+    u32x4_t kept[VPT > 0 ? VPT : 1];
+    if constexpr (VPT > 0) {
+        constexpr bool ONCE = VPT * V <= 16;  // gamma stays in registers
+        float g_kept[ONCE ? VPT : 1][V];
+        auto factors = [&](int i, float* g) {
+            if constexpr (ONCE) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) g[e] = g_kept[i][e];
+            } else {
+                load_gamma(thread + i * THREADS, g);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int v = thread + i * THREADS;
+            kept[i] = v < vectors ? Vec::load(xp + (long long)v * 16, a.c - v * V) : u32x4_t{0, 0, 0, 0};
+        }
+        if (rp) {
+            u32x4_t r[VPT];
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int v = thread + i * THREADS;
+                r[i] = v < vectors ? Vec::load(rp + (long long)v * 16, a.c - v * V) : u32x4_t{0, 0, 0, 0};
+            }
+            if constexpr (ONCE && KIND != kQuantize) {
+#pragma unroll
+                for (int i = 0; i < VPT; ++i)
+                    if (thread + i * THREADS < vectors) load_gamma(thread + i * THREADS, g_kept[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) kept[i] = added(kept[i], r[i]);
+        } else if constexpr (ONCE && KIND != kQuantize) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+                if (thread + i * THREADS < vectors) load_gamma(thread + i * THREADS, g_kept[i]);
+        }
+        double squares = 0.0;
+        unsigned most_of[VPT], most = 0;  // bits of the largest |t| without the sign, twice: NaNs are above infinity
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int v = thread + i * THREADS;
+            most_of[i] = 0;
+            if (v >= vectors) continue;
+            if (hp) Vec::store(hp + (long long)v * 16, kept[i], a.c - v * V);
+            float g[V], sum = 0.f;
+            if constexpr (KIND == kNormI8) factors(i, g);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float h = Vec::get(kept[i], e);
+                if constexpr (KIND != kQuantize) sum = __builtin_fmaf(h, h, sum);
+                if constexpr (KIND != kNorm) most_of[i] = max(most_of[i], __float_as_uint(KIND == kNormI8 ? h * g[e] : h) << 1);
+            }
+            most = max(most, most_of[i]);
+            squares += (double)sum;
+        }
+        if constexpr (KIND != kQuantize) squares = over_wavefront(squares, Add());
+        if constexpr (KIND != kNorm) most = over_wavefront(most, Most());
+        if constexpr (WAVES > 1) {
+            if ((threadIdx.x & 63) == 0) {
+                joined.squares[wave] = squares;
+                joined.bits[wave] = most;
+            }
+            __syncthreads();
+            if constexpr (KIND != kQuantize) squares = over_wavefronts<WAVES>(joined.squares, Add());
+            if constexpr (KIND != kNorm) most = over_wavefronts<WAVES>(joined.bits, Most());
+        }
+        bool fast = KIND == kQuantize || (squares >= 0x1p-60 && squares <= 0x1p120);
+        if constexpr (KIND != kNorm) fast = fast && most >= __float_as_uint(0x1p-90f) << 1 && most <= __float_as_uint(0x1p90f) << 1;
+        fast = __all(fast);
+        if (fast) {
+            float factor = 1.f;
+            double wide = 1.0;
+            if constexpr (KIND != kQuantize) {
+                wide = 1.0 / sqrt(squares / a.c + (double)a.eps);
+                factor = (float)wide;
+            }
+            if constexpr (KIND == kNorm) {
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) {
+                    const int v = thread + i * THREADS;
+                    if (v >= vectors) continue;
+                    float g[V], z[V];
+                    factors(i, g);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) z[e] = Vec::get(kept[i], e) * factor * g[e];
+                    Vec::store(yp + (long long)v * 16, Vec::pack(z), a.c - v * V);
+                }
+                return;
+            }
+            // the largest |t| itself, among what 32 bits have close to it
+            double largest = __uint_as_float(most >> 1);
+            if constexpr (KIND == kNormI8) {
+                largest = 0.0;
+                const unsigned close = most - 8;  // four steps of a 32-bit number: t is off by half of one
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) {
+                    if (most_of[i] < close) continue;
+                    float g[V];
+                    factors(i, g);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) largest = fmax(largest, thread * V + i * THREADS * V + e < a.c ? fabs(in_64_bits(Vec::get(kept[i], e), g[e])) : 0.0);
+                }
+                largest = over_wavefront(largest, Most());
+                if constexpr (WAVES > 1) {
+                    if ((threadIdx.x & 63) == 0) joined.most[wave] = largest;
+                    __syncthreads();
+                    largest = over_wavefronts<WAVES>(joined.most, Most());
+                }
+            }
+            if (thread == 0) a.scales[row] = (float)(largest * wide / 127.0);
+            const float step = (float)(127.0 / largest);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int v = thread + i * THREADS;
+                if (v >= vectors) continue;
+                float g[V], far = 0.f;
+                if constexpr (KIND == kNormI8) factors(i, g);
+                unsigned q[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float h = Vec::get(kept[i], e), u = (KIND == kNormI8 ? h * g[e] : h) * step;
+                    const float placed = u + 0x1.8p23f;  // u, rounded, in the low bits
+                    q[e] = __float_as_uint(placed);
+                    far = fmaxf(far, fabsf(u - (placed - 0x1.8p23f)));
+                }
+                if (far > 0.5f - 0x1p-15f) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) q[e] = integer(in_64_bits(Vec::get(kept[i], e), KIND == kNormI8 ? g[e] : 1.f), largest);
+                }
+                Vec::store_i8(yp + (long long)v * V, q, a.c - v * V);
+            }
+            return;
+        }
+        if constexpr (WAVES > 1) __syncthreads();  // (before the sums are written again)
+    }
+
+    // ---- in 64 bits, where no square of a 32-bit number overflows or vanishes ----
+    double squares = 0.0, most = 0.0;
+    unsigned odd = 0;  // an infinity or a NaN among the t
+    auto stream = [&](int v) {
+        const int live = a.c - v * V;
+        const u32x4_t x = Vec::load(xp + (long long)v * 16, live);
+        return rp ? added(x, Vec::load(rp + (long long)v * 16, live)) : x;
+    };
     auto take = [&](int v, u32x4_t h) {
-        if (hp) Vec::store(hp + (long long)v * 16, h, a.c - v * V);
         float g[V];
         if constexpr (KIND == kNormI8) load_gamma(v, g);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const double f = Vec::get(h, e);
-            if constexpr (KIND != kQuantize) stat.squares = __builtin_fma(f, f, stat.squares);
+            if (v * V + e >= a.c) continue;
+            const double f = Vec::get(h, e), t = KIND == kNormI8 ? f * (double)g[e] : f;
+            if constexpr (KIND != kQuantize) squares = __builtin_fma(f, f, squares);
             if constexpr (KIND != kNorm) {
-                const double t = KIND == kNormI8 ? f * (double)g[e] : f;
-                stat.most = fmax(stat.most, fabs(t));
-                stat.odd |= !(fabs(t) < (double)INFINITY);
+                most = fmax(most, fabs(t));
+                odd |= !(fabs(t) < (double)INFINITY);
             }
         }
     };
-    u32x4_t kept[VPT > 0 ? VPT : 1];
     if constexpr (VPT > 0) {
+#pragma unroll 1
+        for (int i = 0; i < VPT; ++i) {
+            u32x4_t h = kept[0];
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) kept[i] = thread + i * THREADS < vectors ? stream(thread + i * THREADS) : u32x4_t{0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < VPT; ++i)
-            if (thread + i * THREADS < vectors) take(thread + i * THREADS, kept[i]);
+            for (int j = 1; j < VPT; ++j) h = i == j ? kept[j] : h;
+            if (thread + i * THREADS < vectors) take(thread + i * THREADS, h);
+        }
     } else {
-        for (int v = thread; v < vectors; v += THREADS) take(v, stream(v));
+        for (int v = thread; v < vectors; v += THREADS) {
+            const u32x4_t h = stream(v);
+            if (hp) Vec::store(hp + (long long)v * 16, h, a.c - v * V);
+            take(v, h);
+        }
     }
-    stat = join<THREADS>(stat, shared);
-
-    double factor = 1.0;  // 1 / root mean square
-    if constexpr (KIND != kQuantize) factor = 1.0 / sqrt(stat.squares / a.c + (double)a.eps);
-    const bool odd = KIND != kNorm && (stat.odd || !(stat.squares < (double)INFINITY));
+    squares = over_wavefront(squares, Add());
+    most = over_wavefront(most, Most());
+    odd = over_wavefront(odd, Most());
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) {
+            joined.squares[wave] = squares;
+            joined.most[wave] = most;
+            joined.bits[wave] = odd;
+        }
+        __syncthreads();
+        squares = over_wavefronts<WAVES>(joined.squares, Add());
+        most = over_wavefronts<WAVES>(joined.most, Most());
+        odd = over_wavefronts<WAVES>(joined.bits, Most());
+    }
+    double factor = 1.0;
+    if constexpr (KIND != kQuantize) factor = 1.0 / sqrt(squares / a.c + (double)a.eps);
+    if (!(squares < (double)INFINITY)) odd = 1;
     if constexpr (KIND != kNorm) {
-        if (thread == 0) a.scales[row] = odd ? NAN : (float)(stat.most * factor / 127.0);
+        if (thread == 0) a.scales[row] = odd ? NAN : (float)(most * factor / 127.0);
     }
     // h * factor in 32 bits: the factor as a power of two, which takes h to its place, and a number of 1 to 2
-    int power = 0;
-    float scale = 1.f;
-    if constexpr (KIND == kNorm) {
-        const bool fine = factor > 0.0 && factor < (double)INFINITY;
-        power = fine ? ilogb(factor) : 0;
-        scale = (float)(fine ? ldexp(factor, -power) : factor);
-    }
-    const double step = KIND != kNorm && stat.most > 0.0 ? 127.0 / stat.most : 0.0;
+    const bool fine = factor > 0.0 && factor < (double)INFINITY;
+    const int power = fine ? ilogb(factor) : 0;
+    const float scale = (float)(fine ? ldexp(factor, -power) : factor);
     auto finish = [&](int v, u32x4_t h) {
-        const int live = a.c - v * V;
         float g[V];
         load_gamma(v, g);
         if constexpr (KIND == kNorm) {
             float z[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) z[e] = __builtin_amdgcn_ldexpf(Vec::get(h, e), power) * scale * g[e];
-            Vec::store(yp + (long long)v * 16, Vec::pack(z), live);
+            Vec::store(yp + (long long)v * 16, Vec::pack(z), a.c - v * V);
         } else {
-            int q[V];
+            unsigned q[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const double t = KIND == kNormI8 ? (double)Vec::get(h, e) * (double)g[e] : (double)Vec::get(h, e);
-                const double u = t * step, whole = rint(u);
-                // u is off by less than 2^-45: next to a border between two integers the quotient itself decides
-                q[e] = odd ? 0 : (int)(fabs(u - whole) > 0.5 - 0x1p-40 ? rint(127.0 * t / stat.most) : whole);
-            }
-            Vec::store_i8(yp + (long long)v * V, q, live);
+            for (int e = 0; e < V; ++e) q[e] = odd || most == 0.0 ? 0u : integer(in_64_bits(Vec::get(h, e), g[e]), most);
+            Vec::store_i8(yp + (long long)v * V, q, a.c - v * V);
         }
     };
     if constexpr (VPT > 0) {
+#pragma unroll 1
+        for (int i = 0; i < VPT; ++i) {
+            u32x4_t h = kept[0];
 #pragma unroll
-        for (int i = 0; i < VPT; ++i)
-            if (thread + i * THREADS < vectors) finish(thread + i * THREADS, kept[i]);
+            for (int j = 1; j < VPT; ++j) h = i == j ? kept[j] : h;
+            if (thread + i * THREADS < vectors) finish(thread + i * THREADS, h);
+        }
     } else {
         for (int v = thread; v < vectors; v += THREADS) finish(v, hp ? Vec::load(hp + (long long)v * 16, a.c - v * V) : stream(v));
     }
