@@ -3,10 +3,11 @@
 // Bound by the memory.  A row is read once and kept in the registers of a wavefront or a workgroup (rows beyond that are
 // read twice).  With t = h gamma a row's integers are 127 t / max|t|: the norm's factor cancels, so they need no
 // statistics but the maximum, and they are to be those of the definition whatever the order of anything.  So they are
-// worked out in 32 bits, which leaves a quotient off by less than 2^-15, and those within 2^-15 of a border between two
-// integers are decided in 64 bits, in which t is exact.  Rows whose squares or products could leave the range of
+// worked out in 32 bits, which leaves a quotient (up to 127, three roundings) off by less than 2^-15, and those within
+// 2^-15 of a border between two integers are decided in 64 bits, in which t is exact.  Rows whose squares or products could leave the range of
 // 32-bit numbers, and rows that are not finite, go through 64 bits altogether.
 #include <algorithm>
+#include <type_traits>
 
 #include "decode_ops.h"
 
@@ -24,6 +25,7 @@ struct RowArgs {
     int m, c;
     long long ldx, ldr, ldh, ldy;  // bytes
     float eps;
+    double per_channel;            // 1 / c
 };
 
 // Vectors of 16 bytes of a row, of which the last one may be cut; rows at any alignment of their elements.
@@ -115,8 +117,18 @@ struct Most {
 template <class Op, class T> __device__ __forceinline__ T over_wavefront(T v, Op op)
 {
 #if __HIP_DEVICE_COMPILE__
+    if constexpr (sizeof(T) == 4) {  // the 16 lanes of a row by rotations, then rows and halves
+        auto with = [&](auto turn) { v = op(v, __builtin_bit_cast(T, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x120 + decltype(turn)::value, 0xf, 0xf, true))); };
+        with(std::integral_constant<int, 8>());
+        with(std::integral_constant<int, 4>());
+        with(std::integral_constant<int, 2>());
+        with(std::integral_constant<int, 1>());
+        v = op(v, __shfl_xor(v, 16));
+        v = op(v, __shfl_xor(v, 32));
+    } else {
 #pragma unroll
-    for (int x = 32; x; x >>= 1) v = op(v, __shfl_xor(v, x));
+        for (int x = 32; x; x >>= 1) v = op(v, __shfl_xor(v, x));
+    }
 #endif
     return v;
 }
@@ -160,7 +172,11 @@ template <int DT, int KIND, int THREADS, int VPT> __global__ __launch_bounds__(T
         }
     };
     auto in_64_bits = [&](float h, float g) { return KIND == kQuantize ? (double)h : (double)h * (double)g; };
-    auto integer = [&](double t, double most) { return (unsigned)(int)rint(127.0 * t / most); };
+    // 127 t / most, rounded; step: 127 / most, off by less than 2^-49 of it: next to a border the quotient itself decides
+    auto integer = [&](double t, double most, double step) {
+        const double u = t * step, whole = rint(u);
+        return (unsigned)(int)(fabs(u - whole) > 0.5 - 0x1p-40 ? rint(127.0 * t / most) : whole);
+    };
 
     u32x4_t kept[VPT > 0 ? VPT : 1];
     if constexpr (VPT > 0) {
@@ -198,7 +214,7 @@ template <int DT, int KIND, int THREADS, int VPT> __global__ __launch_bounds__(T
             for (int i = 0; i < VPT; ++i)
                 if (thread + i * THREADS < vectors) load_gamma(thread + i * THREADS, g_kept[i]);
         }
-        double squares = 0.0;
+        float lane_squares = 0.f;
         unsigned most_of[VPT], most = 0;  // bits of the largest |t| without the sign, twice: NaNs are above infinity
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
@@ -215,9 +231,11 @@ template <int DT, int KIND, int THREADS, int VPT> __global__ __launch_bounds__(T
                 if constexpr (KIND != kNorm) most_of[i] = max(most_of[i], __float_as_uint(KIND == kNormI8 ? h * g[e] : h) << 1);
             }
             most = max(most, most_of[i]);
-            squares += (double)sum;
+            lane_squares += sum;
         }
-        if constexpr (KIND != kQuantize) squares = over_wavefront(squares, Add());
+        // (eight squares, eight sums, six levels of lanes: off by at most 22 roundings, the factor by half of that)
+        double squares = 0.0;
+        if constexpr (KIND != kQuantize) squares = over_wavefront(lane_squares, Add());
         if constexpr (KIND != kNorm) most = over_wavefront(most, Most());
         if constexpr (WAVES > 1) {
             if ((threadIdx.x & 63) == 0) {
@@ -235,7 +253,9 @@ template <int DT, int KIND, int THREADS, int VPT> __global__ __launch_bounds__(T
             float factor = 1.f;
             double wide = 1.0;
             if constexpr (KIND != kQuantize) {
-                wide = 1.0 / sqrt(squares / a.c + (double)a.eps);
+                const double mean = __builtin_fma(squares, a.per_channel, (double)a.eps);
+                wide = __builtin_amdgcn_rsq(mean);  // 2^-23 or better, of which a step makes 2^-44
+                wide = __builtin_fma(wide * 0.5, __builtin_fma(-mean * wide, wide, 1.0), wide);
                 factor = (float)wide;
             }
             if constexpr (KIND == kNorm) {
@@ -264,15 +284,27 @@ template <int DT, int KIND, int THREADS, int VPT> __global__ __launch_bounds__(T
 #pragma unroll
                     for (int e = 0; e < V; ++e) largest = fmax(largest, thread * V + i * THREADS * V + e < a.c ? fabs(in_64_bits(Vec::get(kept[i], e), g[e])) : 0.0);
                 }
-                largest = over_wavefront(largest, Most());
+                const unsigned long long found = __ballot(largest > 0.0);  // (most often one lane)
+                if (__popcll(found) == 1) {
+                    const int from = __ffsll(found) - 1;
+                    const unsigned long long bits = __builtin_bit_cast(unsigned long long, largest);
+                    largest = __builtin_bit_cast(double, (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)bits, from) |
+                                                             (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(bits >> 32), from) << 32);
+                } else if (found) {
+                    largest = over_wavefront(largest, Most());
+                }
                 if constexpr (WAVES > 1) {
                     if ((threadIdx.x & 63) == 0) joined.most[wave] = largest;
                     __syncthreads();
                     largest = over_wavefronts<WAVES>(joined.most, Most());
                 }
             }
-            if (thread == 0) a.scales[row] = (float)(largest * wide / 127.0);
-            const float step = (float)(127.0 / largest);
+            if (thread == 0) a.scales[row] = (float)(largest * wide * (1.0 / 127.0));
+            double inverse = __builtin_amdgcn_rcp(largest);  // as above
+            inverse = __builtin_fma(inverse, __builtin_fma(-largest, inverse, 1.0), inverse);
+            inverse = __builtin_fma(inverse, __builtin_fma(-largest, inverse, 1.0), inverse);
+            const double exact_step = 127.0 * inverse;
+            const float step = (float)exact_step;
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
                 const int v = thread + i * THREADS;
@@ -289,7 +321,7 @@ template <int DT, int KIND, int THREADS, int VPT> __global__ __launch_bounds__(T
                 }
                 if (far > 0.5f - 0x1p-15f) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) q[e] = integer(in_64_bits(Vec::get(kept[i], e), KIND == kNormI8 ? g[e] : 1.f), largest);
+                    for (int e = 0; e < V; ++e) q[e] = integer(in_64_bits(Vec::get(kept[i], e), KIND == kNormI8 ? g[e] : 1.f), largest, exact_step);
                 }
                 Vec::store_i8(yp + (long long)v * V, q, a.c - v * V);
             }
@@ -359,6 +391,7 @@ template <int DT, int KIND, int THREADS, int VPT> __global__ __launch_bounds__(T
     const bool fine = factor > 0.0 && factor < (double)INFINITY;
     const int power = fine ? ilogb(factor) : 0;
     const float scale = (float)(fine ? ldexp(factor, -power) : factor);
+    const double step = 127.0 / most;
     auto finish = [&](int v, u32x4_t h) {
         float g[V];
         load_gamma(v, g);
@@ -370,7 +403,7 @@ template <int DT, int KIND, int THREADS, int VPT> __global__ __launch_bounds__(T
         } else {
             unsigned q[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) q[e] = odd || most == 0.0 ? 0u : integer(in_64_bits(Vec::get(h, e), g[e]), most);
+            for (int e = 0; e < V; ++e) q[e] = odd || most == 0.0 ? 0u : integer(in_64_bits(Vec::get(h, e), g[e]), most, step);
             Vec::store_i8(yp + (long long)v * V, q, a.c - v * V);
         }
     };
@@ -410,17 +443,23 @@ template <int DT, int KIND, int THREADS, int VPT> static int launch_rows_as(cons
     return SGPRS_OK;
 }
 
+// Threads of a row by its vectors of 16 bytes: so many that a row is two or four vectors of each, since all of them wait for
+// the slowest; a wavefront only where that would leave it idle.  16384 rows of bf16 with residual and 8-bit results, us:
+// 4096 channels by 256 threads 85 (5.5 TB/s), by 64 98, by 512 99; 2048 by 256 46, by 64 52; 1024 by 64 28, by 256 34.
+// 4000 rows of 16384 by 1024 threads 90, by 512 96, by 256 98; one row of 4096 by 256 4.3, by 64 9.3.
 template <int DT, int KIND> static int launch_rows(const RowArgs& a, hipStream_t stream, int cus)
 {
     constexpr int V = RowVec<DT>::V;
     const int vectors = (a.c - 1) / V + 1;
     if (vectors > 8192) return launch_rows_as<DT, KIND, 1024, 0>(a, stream);
-    if (vectors > 2048) return launch_rows_as<DT, KIND, 1024, 8>(a, stream);
-    if (vectors > 1024) return launch_rows_as<DT, KIND, 256, 8>(a, stream);
-    if (a.m < 4 * cus && vectors > 64) return launch_rows_as<DT, KIND, 256, 4>(a, stream);
-    if (vectors > 512) return launch_rows_as<DT, KIND, 64, 16>(a, stream);
-    if (vectors > 128) return launch_rows_as<DT, KIND, 64, 8>(a, stream);
-    return launch_rows_as<DT, KIND, 64, 2>(a, stream);
+    if (vectors > 4096) return launch_rows_as<DT, KIND, 1024, 8>(a, stream);
+    if (vectors > 2048) return launch_rows_as<DT, KIND, 1024, 4>(a, stream);
+    if (vectors > 1536) return launch_rows_as<DT, KIND, 1024, 2>(a, stream);
+    if (vectors > 1024) return launch_rows_as<DT, KIND, 512, 4>(a, stream);
+    if (vectors > 512) return launch_rows_as<DT, KIND, 256, 4>(a, stream);
+    if (vectors > 256) return launch_rows_as<DT, KIND, 256, 2>(a, stream);
+    if (vectors > 128 || (vectors > 64 && a.m < 4 * cus)) return launch_rows_as<DT, KIND, 256, 1>(a, stream);
+    return vectors > 64 ? launch_rows_as<DT, KIND, 64, 2>(a, stream) : launch_rows_as<DT, KIND, 64, 1>(a, stream);
 }
 
 int launch_rms_norm(const sgprs_rms_norm_desc_t& d, const void* x, const void* residual, const float* gamma, void* sum, void* y, float* scales,
@@ -429,7 +468,7 @@ int launch_rms_norm(const sgprs_rms_norm_desc_t& d, const void* x, const void* r
     const long long es = (long long)dtype_size(d.dtype);
     const bool i8 = d.out_dtype == SGPRS_I8;
     const RowArgs a = {(const unsigned char*)x, (const unsigned char*)residual, gamma, (unsigned char*)sum, (unsigned char*)y, scales, d.m, d.c,
-                       d.ldx * es, d.ldr * es, d.ldh * es, i8 ? d.ldy : d.ldy * es, d.eps};
+                       d.ldx * es, d.ldr * es, d.ldh * es, i8 ? d.ldy : d.ldy * es, d.eps, 1.0 / d.c};
     if (d.dtype == SGPRS_BF16) return i8 ? launch_rows<SGPRS_BF16, kNormI8>(a, stream, cus) : launch_rows<SGPRS_BF16, kNorm>(a, stream, cus);
     return i8 ? launch_rows<SGPRS_F32, kNormI8>(a, stream, cus) : launch_rows<SGPRS_F32, kNorm>(a, stream, cus);
 }
@@ -437,7 +476,7 @@ int launch_rms_norm(const sgprs_rms_norm_desc_t& d, const void* x, const void* r
 int launch_quantize(const sgprs_quantize_desc_t& d, const void* x, int8_t* y, float* scales, hipStream_t stream, int cus)
 {
     const RowArgs a = {(const unsigned char*)x, nullptr, nullptr, nullptr, (unsigned char*)y, scales, d.m, d.c,
-                       d.ldx * (long long)dtype_size(d.dtype), 0, 0, d.ldy, 0.f};
+                       d.ldx * (long long)dtype_size(d.dtype), 0, 0, d.ldy, 0.f, 1.0 / d.c};
     return d.dtype == SGPRS_BF16 ? launch_rows<SGPRS_BF16, kQuantize>(a, stream, cus) : launch_rows<SGPRS_F32, kQuantize>(a, stream, cus);
 }
 
