@@ -11,6 +11,8 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <type_traits>
+#include <utility>
 
 #include "attention_tiles.h"
 #include "decode_ops.h"
@@ -82,6 +84,144 @@ struct Runs {
     }
 };
 
+#if __HIP_DEVICE_COMPILE__
+// The running softmax of up to 4 SETS query heads in fp32 over tiles of 32 keys, with the same parts as Running.  MFMAs of 16
+// blocks of 4 x 4 x 1: a block's rows are four keys and its columns four queries, so that few queries leave no column idle
+// (32 x 32 x 2 takes eight times as long for them).  A row of a tile is CHUNKS chunks of four channels.
+//   scores: lane l brings key l % 32 and the even (lanes below 32) or odd chunks; it ends up with the scores of query
+//           l % 4 with keys 4 (l / 4 % 8) + r, half of the channels in each half of the wavefront.
+//   values: a read brings PK keys, CHUNKS lanes each; the weights reach the lanes as row operands, where the instruction
+//           hands those of one block in each group of blocks to all of the group.  Lane l ends up with channels
+//           4 (l % CHUNKS) + e of all four queries, summed over every PK-th key.
+template <int HD, int SETS> struct RunningNarrow {
+    typedef KvTile<SGPRS_F32, HD> Tile;
+    static constexpr int CHUNKS = Tile::CHUNKS, PK = 64 / CHUNKS, GROUP_LOG2 = CHUNKS == 32 ? 3 : CHUNKS == 16 ? 2 : 1;  // blocks of a group
+    static constexpr int Q = CHUNKS / 2;  // vectors of q
+    typedef float f32x4_t __attribute__((ext_vector_type(4)));
+    f32x4_t o[SETS][4];  // [.][e][query]
+    float top[SETS], sum[SETS];
+    unsigned k_place, v_place;
+    __device__ __forceinline__ RunningNarrow()
+    {
+        const int lane = threadIdx.x & 63, row = lane & 31, group = lane / CHUNKS;
+        k_place = LanePlaces<SGPRS_F32, HD>::place(row, lane >> 5);
+        // key of group g at step (block, r): 4 (g * blocks of a group + block) % 32 + r, the upper half one further
+        v_place = LanePlaces<SGPRS_F32, HD>::place((group << (GROUP_LOG2 + 2)) % 32 + (lane >> 5), lane % CHUNKS);
+    }
+    __device__ __forceinline__ void start()
+    {
+#pragma unroll
+        for (int s = 0; s < SETS; ++s) {
+            top[s] = -INFINITY;
+            sum[s] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[s][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    // of query l % 4 of a set, in all lanes
+    __device__ __forceinline__ float total(int s) const
+    {
+        float v = sum[s];
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) v += __shfl_xor(v, x);
+        return v;
+    }
+    // channels 4 (l % CHUNKS) + e of a set's query i, in all lanes
+    __device__ __forceinline__ float4 result(int s, int i) const
+    {
+        float z[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            z[e] = o[s][e][i];
+#pragma unroll
+            for (int x = CHUNKS; x < 64; x <<= 1) z[e] += __shfl_xor(z[e], x);
+        }
+        return make_float4(z[0], z[1], z[2], z[3]);
+    }
+    static __device__ __forceinline__ float of_query(float v, int i)
+    {
+        const int w = __float_as_int(v);
+        switch (i) {
+        case 0: return __int_as_float(__builtin_amdgcn_mov_dpp(w, 0x00, 0xf, 0xf, true));
+        case 1: return __int_as_float(__builtin_amdgcn_mov_dpp(w, 0x55, 0xf, 0xf, true));
+        case 2: return __int_as_float(__builtin_amdgcn_mov_dpp(w, 0xaa, 0xf, 0xf, true));
+        default: return __int_as_float(__builtin_amdgcn_mov_dpp(w, 0xff, 0xf, 0xf, true));
+        }
+    }
+    template <class KDone, class VReady>
+    __device__ __forceinline__ void tile(const u32x4_t (*q)[Q], float scale_log2, unsigned k_at, unsigned v_at, int key0, int first_unseen, KDone k_done, VReady v_ready)
+    {
+        const unsigned k_base = LanePlaces<SGPRS_F32, HD>::hidden(k_place + k_at), v_base = LanePlaces<SGPRS_F32, HD>::hidden(v_place + v_at);
+        f32x4_t s[2 * SETS];  // (two chains of MFMAs that alternate)
+#pragma unroll
+        for (int n = 0; n < 2 * SETS; ++n) s[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < Q; ++c) {
+            const u32x4_t k = *(const lds_u32x4_t*)(unsigned long)(k_base ^ (unsigned)(c << 5));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int n = 0; n < SETS; ++n)
+                    s[e % 2 * SETS + n] = __builtin_amdgcn_mfma_f32_4x4x1f32(__uint_as_float(k[e]), __uint_as_float(q[n][c][e]), s[e % 2 * SETS + n], 0, 0, 0);
+        }
+#pragma unroll
+        for (int n = 0; n < SETS; ++n) s[n] += s[SETS + n];
+        k_done();
+        const int lane = threadIdx.x & 63, mine = first_unseen - key0 - ((lane >> 2) & 7) * 4;
+        float p[SETS][4];
+#pragma unroll
+        for (int n = 0; n < SETS; ++n) {
+            float most = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[n][r] += __shfl_xor(s[n][r], 32);
+                s[n][r] = r < mine ? s[n][r] : -INFINITY;
+                most = fmaxf(most, s[n][r]);
+            }
+            most *= scale_log2;
+            if (__any(most > top[n] + kKeepMax)) {
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) most = fmaxf(most, __shfl_xor(most, x));
+                const float now = fmaxf(top[n], most), keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[n] - now);
+                top[n] = now;
+                sum[n] *= keep;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float k = of_query(keep, i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[n][e][i] *= k;
+                }
+            }
+            const float base = top[n] == -INFINITY ? 0.f : top[n] + kKeepMax;  // weights stay below 1, so sums with large v keep their range
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                p[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], scale_log2, -base));
+                sum[n] += p[n][r];
+            }
+            const float odd0 = p[n][1], odd2 = p[n][3];  // the upper half takes the odd keys
+            if (lane >= 32) {
+                p[n][0] = odd0;
+                p[n][2] = odd2;
+            }
+        }
+        v_ready();
+        all_values(v_base, p, std::make_integer_sequence<int, 1 << GROUP_LOG2>());
+    }
+    template <int... B> __device__ __forceinline__ void all_values(unsigned v_base, const float (*p)[4], std::integer_sequence<int, B...>) { (values<B>(v_base, p), ...); }
+    template <int B> __device__ __forceinline__ void values(unsigned v_base, const float (*p)[4])
+    {
+#pragma unroll
+        for (int r = 0; r < 4; r += 2) {
+            const u32x4_t v = *(const lds_u32x4_t*)(unsigned long)LanePlaces<SGPRS_F32, HD>::plus(v_base, 4 * B + r, 0);
+#pragma unroll
+            for (int n = 0; n < SETS; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n][e] = __builtin_amdgcn_mfma_f32_4x4x1f32(p[n][r], __uint_as_float(v[e]), o[n][e], GROUP_LOG2, B, 0);
+        }
+    }
+};
+#endif
+
 template <int DT, int HD> struct PagedShape {
     static constexpr int HALF = 32 * KvTile<DT, HD>::ROW, STAGE = 2 * HALF;  // k, and v behind it
     static constexpr int SROW = HD + 4;                                       // floats of a row where the sums meet
@@ -99,7 +239,8 @@ struct Segment {
 };
 #endif
 
-template <int DT, int HD> __global__ __launch_bounds__(256, (PagedShape<DT, HD>::PER_CU)) void paged_attention_kernel(const PagedArgs a)
+// SETS: of four heads of a key head, in fp32; 0: up to 32 heads.
+template <int DT, int HD, int SETS> __global__ __launch_bounds__(256, (PagedShape<DT, HD>::PER_CU)) void paged_attention_kernel(const PagedArgs a)
 {
 #if __HIP_DEVICE_COMPILE__
     typedef KvTile<DT, HD> Tile;
@@ -233,12 +374,22 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (PagedShape<DT, HD>:
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (lds_ptr_t)(to + i * 1024), 16, 0, 0);
         }
     };
-    u32x4_t q[STEPS];
+    constexpr int ROWS = SETS > 0 ? SETS : 1, Q = SETS > 0 ? HD * ES / 32 + (HD == 96) * 4 : STEPS;
+    u32x4_t q[ROWS][Q];
     auto load_q = [&](const Segment& s) {
         const int kv_head = kv_head_of(a, s.item), block = quotient(s.item, a.heads_mul, a.heads_sh);
+        if constexpr (SETS > 0) {
+#pragma unroll
+            for (int n = 0; n < SETS; ++n) {
+                const unsigned char* qp = a.q + (long long)s.seq * a.ldq + (kv_head * a.group + min(n * 4 + (lane & 3), a.group - 1)) * a.hq;
+#pragma unroll
+                for (int c = 0; c < Q; ++c) q[n][c] = (2 * c + h) * 16 < row_bytes ? *(const u32x4_t*)(qp + (2 * c + h) * 16) : u32x4_t{0, 0, 0, 0};
+            }
+            return;
+        }
         const unsigned char* qp = a.q + (long long)s.seq * a.ldq + (kv_head * a.group + min(block * 32 + col, a.group - 1)) * a.hq;
 #pragma unroll
-        for (int c = 0; c < STEPS; ++c) q[c] = (2 * c + h) * 16 < row_bytes ? *(const u32x4_t*)(qp + (2 * c + h) * 16) : u32x4_t{0, 0, 0, 0};
+        for (int c = 0; c < Q; ++c) q[0][c] = (2 * c + h) * 16 < row_bytes ? *(const u32x4_t*)(qp + (2 * c + h) * 16) : u32x4_t{0, 0, 0, 0};
     };
 
     Segment now = {}, next = {};
@@ -260,8 +411,10 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (PagedShape<DT, HD>:
             next_entry = entry_of(next, next_t + NW);
         }
 #pragma unroll
-        for (int c = 0; c < STEPS; ++c) q[c] ^= a.q_flip;
-        Running<DT, HD> run;
+        for (int n = 0; n < ROWS; ++n)
+#pragma unroll
+            for (int c = 0; c < Q; ++c) q[n][c] ^= a.q_flip;
+        std::conditional_t<(SETS > 0), RunningNarrow<HD, ROWS>, Running<DT, HD>> run;
         run.start();
         // a tile for each wavefront at least, if only one without keys
         do {
@@ -278,7 +431,9 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (PagedShape<DT, HD>:
                 request(a.k, buffers, place);
             };
             auto v_ready = [&] { landed(std::integral_constant<int, LOADS>()); };  // v, before the next k
-            run.template tile<1, true, true>(q, a.scale_log2, buffers_at, buffers_at + Shape::HALF, t * 32, min(now.n, now.end * 32), k_done, v_ready);
+            const int unseen = min(now.n, now.end * 32);
+            if constexpr (SETS > 0) run.tile(q, a.scale_log2, buffers_at, buffers_at + Shape::HALF, t * 32, unseen, k_done, v_ready);
+            else run.template tile<1, true, true>(q[0], a.scale_log2, buffers_at, buffers_at + Shape::HALF, t * 32, unseen, k_done, v_ready);
             read();
             request(a.v, buffers + Shape::HALF, place);
             t += NW;
@@ -290,7 +445,8 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (PagedShape<DT, HD>:
         const int rows = min(32, a.group - block * 32), first_head = kv_head * a.group + block * 32, vecs = a.head_dim >> 2;
         const bool whole = now.begins() && now.ends();
         const long long part = ((long long)blockIdx.x * 2 + !now.ends()) * a.rows;
-        const float sum = run.total();
+        float sum = 0.f;
+        if constexpr (SETS == 0) sum = run.total();
         float* sums = (float*)(smem + Shape::MEET);  // [wavefront][row][channel], then [wavefront][row] maxima and sums
         float* tops = sums + NW * kMeetRows * Shape::SROW;
         float* sum_of = tops + NW * kMeetRows;
@@ -302,7 +458,22 @@ template <int DT, int HD> __global__ __launch_bounds__(256, (PagedShape<DT, HD>:
         };
         for (int r0 = 0; r0 < rows; r0 += kMeetRows) {
             meet();
-            if (col >= r0 && col < r0 + kMeetRows) {
+            if constexpr (SETS > 0) {
+#pragma unroll
+                for (int n = 0; n < SETS; ++n) {
+                    if (n * 4 != r0) continue;
+                    const float all = run.total(n);
+                    if (lane < 4) {
+                        tops[wave * kMeetRows + lane] = run.top[n];
+                        sum_of[wave * kMeetRows + lane] = all;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float4 z = run.result(n, i);
+                        if (lane < RunningNarrow<HD, ROWS>::CHUNKS && lane * 4 < HD) *(float4*)(sums + (wave * kMeetRows + i) * Shape::SROW + lane * 4) = z;
+                    }
+                }
+            } else if (col >= r0 && col < r0 + kMeetRows) {
                 const int r = wave * kMeetRows + col - r0;
 #pragma unroll
                 for (int d = 0; d < HD / 32; ++d)
@@ -514,11 +685,18 @@ template <auto kernel> static int launch_sized(dim3 grid, int lds, const PagedAr
 template <int DT> static int launch_typed(const PagedArgs& a, const PagedPlan& p, hipStream_t stream)
 {
     const dim3 grid((unsigned)p.workgroups);
+    auto sized = [&](auto sets) {
+        constexpr int SETS = decltype(sets)::value;
+        if (a.head_dim <= 32) return launch_sized<paged_attention_kernel<DT, 32, SETS>>(grid, PagedShape<DT, 32>::LDS, a, stream);
+        if (a.head_dim <= 64) return launch_sized<paged_attention_kernel<DT, 64, SETS>>(grid, PagedShape<DT, 64>::LDS, a, stream);
+        if (a.head_dim <= 96) return launch_sized<paged_attention_kernel<DT, 96, SETS>>(grid, PagedShape<DT, 96>::LDS, a, stream);
+        return launch_sized<paged_attention_kernel<DT, 128, SETS>>(grid, PagedShape<DT, 128>::LDS, a, stream);
+    };
     int rc;
-    if (a.head_dim <= 32) rc = launch_sized<paged_attention_kernel<DT, 32>>(grid, PagedShape<DT, 32>::LDS, a, stream);
-    else if (a.head_dim <= 64) rc = launch_sized<paged_attention_kernel<DT, 64>>(grid, PagedShape<DT, 64>::LDS, a, stream);
-    else if (a.head_dim <= 96) rc = launch_sized<paged_attention_kernel<DT, 96>>(grid, PagedShape<DT, 96>::LDS, a, stream);
-    else rc = launch_sized<paged_attention_kernel<DT, 128>>(grid, PagedShape<DT, 128>::LDS, a, stream);
+    if constexpr (DT == SGPRS_F32)
+        rc = a.group <= 4 ? sized(std::integral_constant<int, 1>()) : a.group <= 8 ? sized(std::integral_constant<int, 2>()) : sized(std::integral_constant<int, 0>());
+    else
+        rc = sized(std::integral_constant<int, 0>());
     if (rc || !p.join) return rc;
     return launch_sized<paged_join_kernel<DT>>(dim3((unsigned)p.workgroups, (unsigned)std::min(p.rows, 8)), 0, a, stream);
 }
