@@ -169,6 +169,49 @@ __device__ __forceinline__ void add_values(f32x16_t* o, const float* p, unsigned
     }
 }
 
+// The same for bf16 with all of a block's fragments read at once.  The reads are inline assembly, waited for inside it: before
+// the builtins' the compiler waits for every load that writes LDS, the next tile's too.
+template <int HD> __device__ __forceinline__ void add_values_at_once(f32x16_t* o, const float* p, unsigned v_base)
+{
+    typedef KvTile<SGPRS_BF16, HD> Tile;
+    constexpr int DB = HD / 32;
+    u32x4_t w[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[u][e] = pack_bf16x2_relu(p[8 * u + 2 * e], p[8 * u + 2 * e + 1], kNoReluFloor);
+#pragma unroll
+    for (int d0 = 0; d0 < DB; d0 += 2) {
+        constexpr int N = DB > 1 ? 2 : 1;
+        u32x2_t f[2][2][2];  // [d][u][a]
+        unsigned at[2][2];
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int a = 0; a < 2; ++a) at[d][a] = LanePlaces<SGPRS_BF16, HD>::plus(v_base, a * 8, (min(d0 + d, DB - 1)) * 4);
+        if constexpr (N == 2)
+            asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9\n\tds_read_b64_tr_b16 %2, %8 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+                         "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %11\n\tds_read_b64_tr_b16 %6, %10 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+                         "s_waitcnt lgkmcnt(0)"
+                         : "=&v"(f[0][0][0]), "=&v"(f[0][0][1]), "=&v"(f[0][1][0]), "=&v"(f[0][1][1]), "=&v"(f[1][0][0]), "=&v"(f[1][0][1]), "=&v"(f[1][1][0]), "=&v"(f[1][1][1])
+                         : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "n"(16 * Tile::ROW)
+                         : "memory");
+        else
+            asm volatile("ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %5\n\tds_read_b64_tr_b16 %2, %4 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%6\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(f[0][0][0]), "=&v"(f[0][0][1]), "=&v"(f[0][1][0]), "=&v"(f[0][1][1])
+                         : "v"(at[0][0]), "v"(at[0][1]), "n"(16 * Tile::ROW)
+                         : "memory");
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (d0 + d >= DB) continue;
+                const u32x4_t v = {f[d][u][0][0], f[d][u][0][1], f[d][u][1][0], f[d][u][1][1]};
+                o[d0 + d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, w[u]), o[d0 + d], 0, 0, 0);
+            }
+    }
+}
+
 // Of a tile's keys, a lane sees those below this, counted from its half's first one.
 __device__ __forceinline__ int keys_left(int key0, int first_unseen)
 {
@@ -274,7 +317,12 @@ template <int DT, int HD> struct Running {
                 p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale_log2, -base));
                 sum += p[i];
             }
-            add_values<DT, HD, MASKED && !ZEROS>(o, p, v_base, b, &odd);
+            if constexpr (ZEROS && DT == SGPRS_BF16) {
+                static_assert(BLOCKS == 1, "a block at a time");
+                add_values_at_once<HD>(o, p, v_base);
+            } else {
+                add_values<DT, HD, MASKED && !ZEROS>(o, p, v_base, b, &odd);
+            }
         }
         if constexpr (MASKED && !ZEROS) {
             static_assert(BLOCKS == 1, "a block at a time");

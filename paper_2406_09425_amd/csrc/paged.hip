@@ -52,7 +52,7 @@ constexpr int kMaxWorkgroups = 2 * SGPRS_MAX_MASK_WORDS * 32;
 constexpr int kItemCost = 1;         // what an item costs beside its units, in units
 constexpr int kMeetRows = 4;         // rows whose sums meet in LDS at once
 
-__device__ __align__(16) unsigned paged_zeros[4] = {0, 0, 0, 0};  // what is loaded for positions behind the last
+__device__ __align__(16) unsigned paged_zeros[128] = {};  // a row that is loaded for positions behind the last
 
 __device__ __forceinline__ int quotient(int n, unsigned mul, int sh) { return (int)(__umulhi(2u * (unsigned)n, mul) >> sh); }
 
@@ -225,7 +225,7 @@ template <int HD, int SETS> struct RunningNarrow {
 template <int DT, int HD> struct PagedShape {
     static constexpr int HALF = 32 * KvTile<DT, HD>::ROW, STAGE = 2 * HALF;  // k, and v behind it
     static constexpr int SROW = HD + 4;                                       // floats of a row where the sums meet
-    static constexpr int MEET = kWaves * STAGE, LDS = MEET + kWaves * kMeetRows * (SROW + 2) * 4;
+    static constexpr int ROWS_AT = kWaves * STAGE, MEET = ROWS_AT + kWaves * 256, LDS = MEET + kWaves * kMeetRows * (SROW + 2) * 4;
     static constexpr int PER_CU = LDS > 81920 ? 1 : 2;
 };
 
@@ -320,7 +320,8 @@ template <int DT, int HD, int SETS> __global__ __launch_bounds__(256, (PagedShap
             if (item == a.items) {
                 item = 0;
                 if (++seq >= a.n_seqs) return false;
-                seen = seen_of(a, a.lens[seq]);
+                // (a scalar load: a vector load's wait would be for the keys on their way, too)
+                seen = seen_of(a, *(const __attribute__((address_space(4))) int*)(unsigned long)(a.lens + seq));
                 item_cost = seen.cost(a);
             }
             const int here = min(run_end - at, item_cost - offset), tiles = max(1, (seen.n + 31) >> 5);
@@ -363,33 +364,49 @@ template <int DT, int HD, int SETS> __global__ __launch_bounds__(256, (PagedShap
         const long long place = page * a.page_stride + in * a.token_stride + kv_head_of(a, s.item) * a.head_stride;
         return t < s.end && t * 32 + col < s.n ? place : -1;
     };
+    // Addresses go through LDS from the lanes that worked them out to those that load: eight bytes a row.
+    typedef __attribute__((address_space(3))) unsigned long long lds_u64_t;
+    const unsigned rows_at = (unsigned)(Shape::ROWS_AT + wave * 256);
+    const bool padded = row_bytes < Tile::ROW;
     auto request = [&](const unsigned char* cache, unsigned char* to, long long place) {
-        int lane_row = lrow;
-        asm volatile("" : "+v"(lane_row));  // what follows from it is worked out in every tile rather than kept in registers
+        *(lds_u64_t*)(unsigned long)(rows_at + col * 8) = (unsigned long long)(place >= 0 ? cache + place : (const unsigned char*)paged_zeros);
+        unsigned from = rows_at + lrow * 8, first = slot << 4;
+        asm volatile("" : "+v"(from), "+v"(first));  // what follows from them is worked out in every tile rather than kept in registers
+        unsigned long long row[LOADS];
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int chunk = (slot ^ Tile::swizzle(i * RPI)) << 4;
-            const long long row = __shfl(place, i * RPI + lane_row);
-            const unsigned char* p = row >= 0 && chunk < row_bytes ? cache + row + chunk : (const unsigned char*)paged_zeros;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (lds_ptr_t)(to + i * 1024), 16, 0, 0);
+        for (int i = 0; i < LOADS; ++i) row[i] = *(const lds_u64_t*)(unsigned long)(from + i * RPI * 8);
+        if (padded) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int chunk = first ^ (Tile::swizzle(i * RPI) << 4);
+                row[i] = chunk < row_bytes ? row[i] + chunk : (unsigned long long)paged_zeros;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) row[i] += first ^ (Tile::swizzle(i * RPI) << 4);
         }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)row[i], (lds_ptr_t)(to + i * 1024), 16, 0, 0);
     };
     constexpr int ROWS = SETS > 0 ? SETS : 1, Q = SETS > 0 ? HD * ES / 32 + (HD == 96) * 4 : STEPS;
     u32x4_t q[ROWS][Q];
+    auto load_row = [&](u32x4_t* to, const unsigned char* from) {
+#pragma unroll
+        for (int c = 0; c < Q; ++c) to[c] = *(const u32x4_t*)(padded && (2 * c + h) * 16 >= row_bytes ? (const unsigned char*)paged_zeros : from + (2 * c + h) * 16);
+    };
     auto load_q = [&](const Segment& s) {
         const int kv_head = kv_head_of(a, s.item), block = quotient(s.item, a.heads_mul, a.heads_sh);
         if constexpr (SETS > 0) {
 #pragma unroll
             for (int n = 0; n < SETS; ++n) {
                 const unsigned char* qp = a.q + (long long)s.seq * a.ldq + (kv_head * a.group + min(n * 4 + (lane & 3), a.group - 1)) * a.hq;
-#pragma unroll
-                for (int c = 0; c < Q; ++c) q[n][c] = (2 * c + h) * 16 < row_bytes ? *(const u32x4_t*)(qp + (2 * c + h) * 16) : u32x4_t{0, 0, 0, 0};
+                load_row(q[n], qp);
             }
             return;
         }
         const unsigned char* qp = a.q + (long long)s.seq * a.ldq + (kv_head * a.group + min(block * 32 + col, a.group - 1)) * a.hq;
-#pragma unroll
-        for (int c = 0; c < Q; ++c) q[0][c] = (2 * c + h) * 16 < row_bytes ? *(const u32x4_t*)(qp + (2 * c + h) * 16) : u32x4_t{0, 0, 0, 0};
+        load_row(q[0], qp);
     };
 
     Segment now = {}, next = {};
@@ -447,9 +464,16 @@ template <int DT, int HD, int SETS> __global__ __launch_bounds__(256, (PagedShap
         const long long part = ((long long)blockIdx.x * 2 + !now.ends()) * a.rows;
         float sum = 0.f;
         if constexpr (SETS == 0) sum = run.total();
-        float* sums = (float*)(smem + Shape::MEET);  // [wavefront][row][channel], then [wavefront][row] maxima and sums
-        float* tops = sums + NW * kMeetRows * Shape::SROW;
-        float* sum_of = tops + NW * kMeetRows;
+        // [wavefront][row][channel], then [wavefront][row] maxima and sums: by numbers, since before LDS accesses through
+        // pointers the compiler waits for every load that writes LDS, the next tile's too
+        typedef __attribute__((address_space(3))) float lds_f32_t;
+        typedef __attribute__((address_space(3))) u32x4_t lds_vec_t;
+        auto sums = [](int r) { return (unsigned)(Shape::MEET + r * Shape::SROW * 4); };
+        auto tops = [](int r) { return (lds_f32_t*)(unsigned long)(unsigned)(Shape::MEET + NW * kMeetRows * Shape::SROW * 4 + r * 4); };
+        auto sum_of = [&](int r) { return tops(NW * kMeetRows + r); };
+        auto put = [&](int r, int c, float x, float y, float z, float w) {
+            *(lds_vec_t*)(unsigned long)(sums(r) + c * 4) = u32x4_t{__float_as_uint(x), __float_as_uint(y), __float_as_uint(z), __float_as_uint(w)};
+        };
         auto meet = [] {  // (without waiting for what is on its way from memory)
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_waitcnt(0xC07F);
@@ -464,13 +488,13 @@ template <int DT, int HD, int SETS> __global__ __launch_bounds__(256, (PagedShap
                     if (n * 4 != r0) continue;
                     const float all = run.total(n);
                     if (lane < 4) {
-                        tops[wave * kMeetRows + lane] = run.top[n];
-                        sum_of[wave * kMeetRows + lane] = all;
+                        *tops(wave * kMeetRows + lane) = run.top[n];
+                        *sum_of(wave * kMeetRows + lane) = all;
                     }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float4 z = run.result(n, i);
-                        if (lane < RunningNarrow<HD, ROWS>::CHUNKS && lane * 4 < HD) *(float4*)(sums + (wave * kMeetRows + i) * Shape::SROW + lane * 4) = z;
+                        if (lane < RunningNarrow<HD, ROWS>::CHUNKS && lane * 4 < HD) put(wave * kMeetRows + i, lane * 4, z.x, z.y, z.z, z.w);
                     }
                 }
             } else if (col >= r0 && col < r0 + kMeetRows) {
@@ -479,26 +503,24 @@ template <int DT, int HD, int SETS> __global__ __launch_bounds__(256, (PagedShap
                 for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
                     for (int i = 0; i < 16; i += 4)
-                        *(float4*)(sums + r * Shape::SROW + d * 32 + (i >> 2) * 8 + h * 4) = make_float4(run.o[d][i], run.o[d][i + 1], run.o[d][i + 2], run.o[d][i + 3]);
-                tops[r] = run.top;
-                sum_of[r] = sum;
+                        put(r, d * 32 + (i >> 2) * 8 + h * 4, run.o[d][i], run.o[d][i + 1], run.o[d][i + 2], run.o[d][i + 3]);
+                *tops(r) = run.top;
+                *sum_of(r) = sum;
             }
             meet();
             for (int e = threadIdx.x; e < min(kMeetRows, rows - r0) * 32; e += NW * 64) {
                 const int r = e >> 5, c = (e & 31) * 4;
                 if (c >= a.head_dim) continue;
-                float top = tops[r], total = 0.f, z[4] = {};
+                float top = *tops(r), total = 0.f, z[4] = {};
 #pragma unroll
-                for (int v = 1; v < NW; ++v) top = fmaxf(top, tops[v * kMeetRows + r]);
+                for (int v = 1; v < NW; ++v) top = fmaxf(top, *tops(v * kMeetRows + r));
 #pragma unroll
                 for (int v = 0; v < NW; ++v) {
-                    const float m = tops[v * kMeetRows + r], w = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);  // (both may be -inf: sums of 0)
-                    total = __builtin_fmaf(sum_of[v * kMeetRows + r], w, total);
-                    const float4 o = *(const float4*)(sums + (v * kMeetRows + r) * Shape::SROW + c);
-                    z[0] = __builtin_fmaf(o.x, w, z[0]);
-                    z[1] = __builtin_fmaf(o.y, w, z[1]);
-                    z[2] = __builtin_fmaf(o.z, w, z[2]);
-                    z[3] = __builtin_fmaf(o.w, w, z[3]);
+                    const float m = *tops(v * kMeetRows + r), w = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);  // (both may be -inf: sums of 0)
+                    total = __builtin_fmaf(*sum_of(v * kMeetRows + r), w, total);
+                    const u32x4_t o = *(const lds_vec_t*)(unsigned long)(sums(v * kMeetRows + r) + c * 4);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) z[x] = __builtin_fmaf(__uint_as_float(o[x]), w, z[x]);
                 }
                 if (whole) {
                     const float inv = normaliser(total, now.n > 0);
@@ -524,64 +546,58 @@ template <int DT, int HD, int SETS> __global__ __launch_bounds__(256, (PagedShap
 #endif
 }
 
-// Joins what begins in workgroup blockIdx.x of the first launch and ends in another: 32 lanes of four channels, eight
-// partial sums at a time.
+// Joins what begins in the run of workgroup blockIdx.x and ends in another's: 32 lanes of four channels take every eighth
+// partial sum, each with its maximum (so that both are asked for at once), and meet in a fixed order.
 template <int DT> __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a)
 {
 #if __HIP_DEVICE_COMPILE__
-    __shared__ float weights[kMaxWorkgroups];
-    __shared__ float stat[8];
     __shared__ float4 parts[8][32];
+    __shared__ float tops[8], totals[8];
     const JoinRecord record = a.records[blockIdx.x];
     if (record.last < 0) return;
     const int n = record.last - (int)blockIdx.x + 1;
     const int kv_head = kv_head_of(a, record.item), block = quotient(record.item, a.heads_mul, a.heads_sh), rows = min(32, a.group - block * 32);
-    const int tid = threadIdx.x, lane = tid & 31, group = tid >> 5, c = lane * 4;
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, c = min(lane * 4, a.head_dim - 4);
     for (int r = blockIdx.y; r < rows; r += gridDim.y) {
-        auto part = [&](int p) { return ((long long)(blockIdx.x + p) * 2 + (p != n - 1)) * a.rows + r; };
-        float top = -INFINITY, total = 0.f;
-        for (int p = tid; p < n; p += 256) top = fmaxf(top, a.part_stat[part(p)].x);
+        float top = -INFINITY, total = 0.f, z[4] = {};
+        auto add = [&](float2 stat, float4 o) {
+            const float now = fmaxf(top, stat.x), keep = top == now ? 1.f : __builtin_amdgcn_exp2f(top - now), w = stat.x == now ? 1.f : __builtin_amdgcn_exp2f(stat.x - now);
+            top = now;
+            total = __builtin_fmaf(total, keep, stat.y * w);
+            z[0] = __builtin_fmaf(z[0], keep, o.x * w);
+            z[1] = __builtin_fmaf(z[1], keep, o.y * w);
+            z[2] = __builtin_fmaf(z[2], keep, o.z * w);
+            z[3] = __builtin_fmaf(z[3], keep, o.w * w);
+        };
+        constexpr int AHEAD = 4;
+        for (int p0 = group; p0 < n; p0 += 8 * AHEAD) {
+            float2 stat[AHEAD];
+            float4 o[AHEAD];
 #pragma unroll
-        for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-        if ((tid & 63) == 0) stat[tid >> 6] = top;
-        __syncthreads();
-        top = fmaxf(fmaxf(stat[0], stat[1]), fmaxf(stat[2], stat[3]));
-        for (int p = tid; p < n; p += 256) {
-            const float2 st = a.part_stat[part(p)];
-            const float w = st.x == top ? 1.f : __builtin_amdgcn_exp2f(st.x - top);
-            weights[p] = w;
-            total = __builtin_fmaf(st.y, w, total);
-        }
-#pragma unroll
-        for (int x = 32; x; x >>= 1) total += __shfl_xor(total, x);
-        if ((tid & 63) == 0) stat[4 + (tid >> 6)] = total;
-        __syncthreads();
-        total = (stat[4] + stat[5]) + (stat[6] + stat[7]);
-        float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c < a.head_dim) {
-#pragma unroll 4
-            for (int p = group; p < n; p += 8) {
-                const float w = weights[p];
-                const float4 o = *(const float4*)(a.part_o + part(p) * a.head_dim + c);
-                z = make_float4(__builtin_fmaf(o.x, w, z.x), __builtin_fmaf(o.y, w, z.y), __builtin_fmaf(o.z, w, z.z), __builtin_fmaf(o.w, w, z.w));
+            for (int e = 0; e < AHEAD; ++e) {
+                const int p = min(p0 + e * 8, n - 1);
+                const long long part = ((long long)(blockIdx.x + p) * 2 + (p != n - 1)) * a.rows + r;
+                stat[e] = a.part_stat[part];
+                o[e] = *(const float4*)(a.part_o + part * a.head_dim + c);
             }
-        }
-        parts[group][lane] = z;
-        __syncthreads();
-        if (group == 0 && c < a.head_dim) {
-            float out[4] = {z.x, z.y, z.z, z.w};
 #pragma unroll
-            for (int g = 1; g < 8; ++g) {
-                const float4 t = parts[g][lane];
-                out[0] += t.x;
-                out[1] += t.y;
-                out[2] += t.z;
-                out[3] += t.w;
-            }
+            for (int e = 0; e < AHEAD; ++e)
+                if (p0 + e * 8 < n) add(stat[e], o[e]);
+        }
+        parts[group][lane] = make_float4(z[0], z[1], z[2], z[3]);
+        if (lane == 0) {
+            tops[group] = top;
+            totals[group] = total;
+        }
+        __syncthreads();
+        if (group == 0 && lane * 4 < a.head_dim) {
+#pragma unroll
+            for (int g = 1; g < 8; ++g)
+                if (g < n) add(make_float2(tops[g], totals[g]), parts[g][lane]);
             const float inv = normaliser(total, true);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) out[e] *= inv;
-            store4<DT>(a.o + (long long)record.seq * a.ldo + (kv_head * a.group + block * 32 + r) * a.ho, c, out);
+            for (int e = 0; e < 4; ++e) z[e] *= inv;
+            store4<DT>(a.o + (long long)record.seq * a.ldo + (kv_head * a.group + block * 32 + r) * a.ho, c, z);
         }
         __syncthreads();
     }
