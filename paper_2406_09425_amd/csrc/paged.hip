@@ -42,8 +42,8 @@ struct PagedArgs {
     unsigned heads_mul, grid_mul;
     int heads_sh, grid_sh;           // item / kv_heads, cost / workgroups
     int unit_log2;                   // tiles of a unit
-    float* part_o;                   // [workgroup][ended, not ended][row][head_dim], weights relative to part_stat
-    float2* part_stat;               // [workgroup][ended, not ended][row]: maximum, sum
+    float* part_o;                   // [workgroup][item that goes on, item that begins][row][head_dim], weights relative to part_stat
+    float2* part_stat;               // [workgroup][item that goes on, item that begins][row]: maximum, sum
     JoinRecord* records;             // [workgroup]
 };
 
@@ -461,7 +461,7 @@ template <int DT, int HD, int SETS> __global__ __launch_bounds__(256, (PagedShap
         const int kv_head = kv_head_of(a, now.item), block = quotient(now.item, a.heads_mul, a.heads_sh);
         const int rows = min(32, a.group - block * 32), first_head = kv_head * a.group + block * 32, vecs = a.head_dim >> 2;
         const bool whole = now.begins() && now.ends();
-        const long long part = ((long long)blockIdx.x * 2 + !now.ends()) * a.rows;
+        const long long part = ((long long)blockIdx.x * 2 + now.begins()) * a.rows;
         float sum = 0.f;
         if constexpr (SETS == 0) sum = run.total();
         // [wavefront][row][channel], then [wavefront][row] maxima and sums: by numbers, since before LDS accesses through
@@ -547,17 +547,21 @@ template <int DT, int HD, int SETS> __global__ __launch_bounds__(256, (PagedShap
 }
 
 // Joins what begins in the run of workgroup blockIdx.x and ends in another's: 32 lanes of four channels take every eighth
-// partial sum, each with its maximum (so that both are asked for at once), and meet in a fixed order.
+// partial sum, each with its maximum, and meet in a fixed order.  The first of each are asked for before it is known whether
+// there is something to join.
 template <int DT> __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a)
 {
 #if __HIP_DEVICE_COMPILE__
     __shared__ float4 parts[8][32];
     __shared__ float tops[8], totals[8];
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, c = min(lane * 4, a.head_dim - 4);
+    auto part = [&](int p, int r) { return (min((int)blockIdx.x + p, (int)gridDim.x - 1) * 2ll + (p == 0)) * a.rows + r; };
     const JoinRecord record = a.records[blockIdx.x];
+    const float2 first_stat = a.part_stat[part(group, blockIdx.y)];
+    const float4 first = *(const float4*)(a.part_o + part(group, blockIdx.y) * a.head_dim + c);
     if (record.last < 0) return;
     const int n = record.last - (int)blockIdx.x + 1;
     const int kv_head = kv_head_of(a, record.item), block = quotient(record.item, a.heads_mul, a.heads_sh), rows = min(32, a.group - block * 32);
-    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, c = min(lane * 4, a.head_dim - 4);
     for (int r = blockIdx.y; r < rows; r += gridDim.y) {
         float top = -INFINITY, total = 0.f, z[4] = {};
         auto add = [&](float2 stat, float4 o) {
@@ -570,15 +574,19 @@ template <int DT> __global__ __launch_bounds__(256) void paged_join_kernel(const
             z[3] = __builtin_fmaf(z[3], keep, o.w * w);
         };
         constexpr int AHEAD = 4;
-        for (int p0 = group; p0 < n; p0 += 8 * AHEAD) {
+        int p0 = group;
+        if (r == (int)blockIdx.y) {
+            if (group < n) add(first_stat, first);
+            p0 += 8;
+        }
+        for (; p0 < n; p0 += 8 * AHEAD) {
             float2 stat[AHEAD];
             float4 o[AHEAD];
 #pragma unroll
             for (int e = 0; e < AHEAD; ++e) {
-                const int p = min(p0 + e * 8, n - 1);
-                const long long part = ((long long)(blockIdx.x + p) * 2 + (p != n - 1)) * a.rows + r;
-                stat[e] = a.part_stat[part];
-                o[e] = *(const float4*)(a.part_o + part * a.head_dim + c);
+                const long long at = part(min(p0 + e * 8, n - 1), r);
+                stat[e] = a.part_stat[at];
+                o[e] = *(const float4*)(a.part_o + at * a.head_dim + c);
             }
 #pragma unroll
             for (int e = 0; e < AHEAD; ++e)
