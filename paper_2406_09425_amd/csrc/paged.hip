@@ -677,11 +677,16 @@ static PagedPlan plan_paged(const sgprs_paged_attention_desc_t& d, int cus)
     long long most = (long long)d.table_width * d.page_size;  // positions that a token can see
     if (d.window > 0) most = std::min(most, (long long)d.window + d.sinks);
     const long long tiles = std::max(1ll, (most + 31) / 32), items = (long long)d.n_seqs * d.kv_heads * p.row_blocks;
-    p.unit_log2 = 2;  // a tile for each wavefront; more where the cost of all items could pass 2^31
+    const bool wide = d.dtype == SGPRS_F32 && d.head_dim > 64;  // (LDS for one workgroup of a CU)
+    const long long slots = std::min(kMaxWorkgroups, (wide ? 1 : 2) * cus);
+    // A tile for each wavefront; more where the cost of all items could pass 2^31.  Items of at most 512 keys that have a
+    // workgroup each, and are half of the CUs or more, stay whole, which saves the join: 32/8 heads x 128 in bf16, 128 items of
+    // 300 keys 14.1 -> 10.2 us, 256 of 300 16.7 -> 11.8, of 1 to 512 16.7 -> 12.7, one of 512 and 255 of 60 12.5 -> 10.8; in
+    // fp32 256 of 300 20.2 -> 18.7.  Fewer or longer ones lose by it: 64 items, one of 512 10.0 -> 11.0, 128 of 2048 34 -> 40.
+    p.unit_log2 = tiles <= 16 && items * 2 >= cus && items <= slots ? 4 : 2;
     while (items * (((tiles - 1) >> p.unit_log2) + 1 + kItemCost) >= (1ll << 31)) ++p.unit_log2;
     const long long units = ((tiles - 1) >> p.unit_log2) + 1;
-    const bool wide = d.dtype == SGPRS_F32 && d.head_dim > 64;
-    p.workgroups = (int)std::min<long long>(std::min(kMaxWorkgroups, (wide ? 1 : 2) * cus), items * (units + kItemCost));
+    p.workgroups = (int)std::min(slots, units > 1 ? items * (units + kItemCost) : items);
     p.join = units > 1;
     return p;
 }

@@ -62,6 +62,7 @@ for kind in ("append", "attention"):
                 (kind, dict(head_dim=136), -5), (kind, dict(head_dim=0), -1), (kind, dict(n_pages=0), -1), (kind, dict(page_size=0), -1), (kind, dict(table_width=-1), -1),
                 (kind, dict(table_width=1 << 20, page_size=1025), -5), (kind, dict(token_stride=60), -1), (kind, dict(token_stride=132), -5), (kind, dict(head_stride=1 << 50), -5),
                 (kind, dict(token_stride=64), -1), (kind, dict(page_stride=16 * 128 - 8), -1), (kind, dict(head_stride=128), -1), (kind, dict(page_stride=-2048), -1)]
+REFUSED += [("attention", dict(n_seqs=1 << 17, heads=4098, kv_heads=2049), -5), ("attention", dict(n_seqs=1 << 20, heads=32 * 257, kv_heads=1), -5)]
 REFUSED += [("append", dict(total=-1), -1), ("append", dict(total=(1 << 30) + 1), -5), ("append", dict(ldk=56), -1), ("append", dict(hv=68), -5),
             ("append", dict(ldv=1 << 21), -5), ("attention", dict(heads=3), -1), ("attention", dict(heads=0), -1), ("attention", dict(heads=65536), -5),
             ("attention", dict(window=-1), -1), ("attention", dict(sinks=-1, window=4), -1), ("attention", dict(sinks=1), -1), ("attention", dict(scale=math.nan), -1),

@@ -284,6 +284,34 @@ def test_linear_on_top_of_the_residual(pools, m):
         run_linear(pools, name, m, 130, 260, act=1, res=True, first=1, inplace=True, pads=(0, 0, 6, 6), seed=m)
 
 
+def test_rows_behind_four_gigabytes(pools):
+    """The last rows of a norm and a product whose operands pass 2^32 bytes (repeated rows: what is before them is the same)."""
+    pool, m, c = pools(), (1 << 26) + 67, 72
+    g = gen(6)
+    few = torch.randn(67, c, generator=g).bfloat16()
+    x = few.cuda().repeat((m + 66) // 67, 1)[:m].contiguous()
+    q8, sx = torch.zeros(m, c, dtype=torch.int8, device="cuda"), torch.zeros(m, device="cuda")
+    torch.cuda.synchronize()
+    S.sgprs_rms_norm(S.RmsNormDesc(m=m, c=c, dtype=1, out_dtype=2, eps=1e-6), ptr(x), None, None, None, ptr(q8), ptr(sx), pool, 0)
+    pool.sync()
+    want = ref.rms_norm(few, None, None, 1e-6, True)
+    rows = torch.arange(m - 200, m)
+    same(q8[m - 200:], want[1][rows % 67], "last rows")
+    assert torch.equal(bits(q8[:67 * 1000000].view(1000000, 67, c)), bits(q8[:67].expand(1000000, 67, c).contiguous()))
+    S.sgprs_quantize_i8(S.QuantizeDesc(m=m, c=c, dtype=1), ptr(x), ptr(q8), ptr(sx), pool, 0)
+    pool.sync()
+    want, ws = ref.quantize(few)
+    same(q8[m - 200:], want[rows % 67], "last rows")
+    w = torch.randint(-127, 128, (40, c), generator=g, dtype=torch.int8)
+    gw, y = w.cuda(), torch.zeros(m, 40, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    S.sgprs_linear_i8(S.LinearI8Desc(m=m, n=40, k=c, dtype=1), ptr(q8), ptr(sx), ptr(gw), None, None, None, ptr(y), None, 0, pool, 0)
+    pool.sync()
+    got, bound = ref.linear_i8(want, sx[:67].cpu(), w, None, None, None, 0, 0, torch.bfloat16)
+    block_ops_util.assert_within(y[m - 200:], got[rows % 67], bound[rows % 67], "last rows")
+    assert torch.equal(bits(y[:67 * 1000000].view(1000000, 67, 40)), bits(y[:67].expand(1000000, 67, 40).contiguous()))
+
+
 # ---- paged cache ---------------------------------------------------------------------------------
 class Cache:
     """Caches of n_pages pages; layout: the order of the page's positions and heads."""
@@ -435,6 +463,53 @@ def test_attention_of_many_sequences(pools, name, n):
     kv = torch.randint(0, 40, (n,), generator=g).tolist()
     kv[n // 3], kv[-1], kv[0] = 1500, 300, 0
     run_attention(pools, name, kv, 2, 1, 32, page=8, seed=n)
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,hk,dim", [(2, 1, 32), (3, 1, 128), (5, 1, 64), (8, 1, 24), (14, 2, 128), (16, 2, 96), (9, 1, 32), (16, 1, 128)])
+def test_attention_of_few_heads_of_a_key_head(pools, name, heads, hk, dim):
+    run_attention(pools, name, [333, 64, 1, 0, 130], heads, hk, dim, seed=heads + dim)
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("n,hk,dim,most", [(127, 1, 64, 512), (128, 1, 64, 512), (128, 1, 64, 513), (64, 2, 128, 512), (128, 2, 128, 512), (129, 2, 128, 512), (257, 2, 32, 300), (256, 2, 32, 300)])
+def test_attention_of_items_that_have_a_workgroup_each(pools, name, n, hk, dim, most):
+    """On both sides of where a sequence's keys are no longer split, with equal and different lengths."""
+    kv = torch.randint(0, most + 1, (n,), generator=gen(n + most)).tolist()
+    kv[0], kv[n // 2] = most, 0
+    run_attention(pools, name, kv, 2 * hk, hk, dim, seed=n)
+    run_attention(pools, name, [most] * n, 2 * hk, hk, dim, seed=n)
+
+
+@pytest.mark.parametrize("strides", [dict(page_stride=(1 << 27) + 8, token_stride=256, head_stride=128), dict(page_stride=16 * 128, token_stride=128, head_stride=(1 << 32) + 16),
+                                     dict(page_stride=16 << 20, token_stride=1 << 20, head_stride=128)], ids=["page", "head", "token"])
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_append_and_attention_of_places_far_apart(pools, name, strides):
+    """Offsets that pass 32 bits."""
+    dt, tdt = DT[name]
+    c = Cache(name, [300, 0, 17, 130], 16, 2, 128, seed=4)
+    last = (c.n_pages - 1) * strides["page_stride"] + 15 * strides["token_stride"] + strides["head_stride"] + 128
+    bufs = [torch.empty(last, dtype=tdt, device="cuda") for _ in range(2)]
+    view = [b.as_strided((c.n_pages, 16, 2, 128), (strides["page_stride"], strides["token_stride"], strides["head_stride"], 1)) for b in bufs]
+    c.to_gpu()
+    for at, t in zip(view, (c.gk, c.gv)):
+        at.copy_(t)
+    dims = {**c.dims, **strides}
+    new = [torch.randn(4, 256, generator=gen(i)).to(tdt) for i in (1, 2)]
+    q = torch.randn(4, 512, generator=gen(3)).to(tdt)
+    gnew, gq, o = [t.cuda() for t in new], q.cuda(), torch.empty(4, 512, dtype=tdt, device="cuda")
+    da, dt_ = S.PagedAppendDesc(total=4, **dims), S.PagedAttentionDesc(heads=4, **dims)
+    need = S.sgprs_paged_attention_workspace(dt_, CUS)
+    ws, pool = torch.empty(need, dtype=torch.uint8, device="cuda"), pools()
+    torch.cuda.synchronize()
+    S.sgprs_paged_append(da, ptr(gnew[0]), ptr(gnew[1]), None, ptr(c.gtable), ptr(c.glens), ptr(bufs[0]), ptr(bufs[1]), pool, 0)
+    S.sgprs_paged_attention(dt_, ptr(gq), ptr(bufs[0]), ptr(bufs[1]), ptr(c.gtable), ptr(c.glens), ptr(o), ptr(ws), need, pool, 0)
+    pool.sync()
+    k, v = ref.paged_append(*(t.view(4, 2, 128) for t in new), None, c.table, c.lens.tolist(), *c.host())
+    for at, want in zip(view, (k, v)):
+        assert torch.equal(bits(at.cpu()), bits(want))
+    want, bound = ref.paged_attention(q.view(4, 4, 128), k, v, c.table, c.lens.tolist(), 0, 0, 0.0)
+    block_ops_util.assert_within(o.view(4, 4, 128), want, bound, f"{name} {strides}")
 
 
 def test_attention_of_a_long_cache(pools):
