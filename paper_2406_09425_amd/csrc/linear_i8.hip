@@ -6,6 +6,7 @@
 // and exact, so any split of k gives the same bits.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "decode_ops.h"
 #include "linear_tiles.h"
@@ -37,6 +38,7 @@ __device__ __forceinline__ i32x4_t mma(u32x4_t a, u32x4_t b, i32x4_t c)
 // What belongs to V neighbouring columns (behind the last one: the last one's).
 template <int V> struct Columns {
     float scale[V], bias[V];
+    __device__ __forceinline__ Columns() {}
     __device__ __forceinline__ Columns(const LinearI8Args& a, int col)
     {
 #pragma unroll
@@ -126,14 +128,41 @@ template <int DT, int TN> struct StagedRows {
     static constexpr int V = DT == SGPRS_BF16 ? 8 : 4, PITCH = TN * 16 + 4;  // values of a staged row
     static constexpr int BYTES = 16 * PITCH * 4;
 };
-template <int DT, int ACT, int TM, int TN>
-__device__ __forceinline__ void store_tile(const LinearI8Args& a, const i32x4_t (&acc)[TN][TM], int* mine, long long m0, int n0)
+// What a wavefront's outputs need beside the sums, if it is asked for before they are there: that of the columns and, of a
+// tile that lies inside, row scales and the residual.
+template <int DT, int TM, int TN> struct Ahead {
+    static constexpr int V = StagedRows<DT, TN>::V, ES = 16 / V, LPR = TN * 16 / V, RPP = 64 / LPR, PASSES = 16 / RPP;  // lanes of a row, rows of a pass
+    Columns<V> columns;
+    u32x4_t r[TM][PASSES];
+    float scale[TM][PASSES];
+    __device__ __forceinline__ Ahead(const LinearI8Args& a, long long m0, int n0) : columns(a, n0 + (int)(threadIdx.x & 63) % LPR * V)
+    {
+        if (m0 + 16 * TM > a.m || n0 + 16 * TN > a.n) return;
+        const int lane = threadIdx.x & 63;
+        const unsigned char* rp = a.residual + (m0 + lane / LPR) * a.ldr + (long long)(n0 + lane % LPR * V) * ES;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) {
+                r[i][p] = u32x4_t{0, 0, 0, 0};
+                if (a.residual) __builtin_memcpy(&r[i][p], rp + (long long)(i * 16 + p * RPP) * a.ldr, 16);
+                scale[i][p] = row_scale(a, m0 + i * 16 + p * RPP + lane / LPR);
+            }
+    }
+};
+struct NotAhead {};
+
+template <int DT, int ACT, int TM, int TN, class A>
+__device__ __forceinline__ void store_tile(const LinearI8Args& a, const i32x4_t (&acc)[TN][TM], int* mine, long long m0, int n0, const A& ahead)
 {
 #if __HIP_DEVICE_COMPILE__
+    constexpr bool AHEAD = !std::is_same_v<A, NotAhead>;
     constexpr int V = StagedRows<DT, TN>::V, ES = 16 / V, PITCH = StagedRows<DT, TN>::PITCH;
     constexpr int LPR = TN * 16 / V, RPP = 64 / LPR, PASSES = 16 / RPP;  // lanes of a row, rows of a pass
     const int lane = threadIdx.x & 63, frow = lane & 15, fgrp = lane >> 4, r0 = lane / LPR, c0 = lane % LPR * V, col = n0 + c0;
-    const Columns<V> columns(a, col);
+    Columns<V> columns;
+    if constexpr (AHEAD) columns = ahead.columns;
+    else columns = Columns<V>(a, col);
     auto stage = [&](auto i) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) *(i32x4_t*)(mine + frow * PITCH + j * 16 + fgrp * 4) = acc[j][i];
@@ -154,12 +183,19 @@ __device__ __forceinline__ void store_tile(const LinearI8Args& a, const i32x4_t 
         for_each<TM>([&](auto i) {
             u32x4_t r[PASSES] = {};
             float scale[PASSES];
-            if (a.residual) {
+            if (!AHEAD && a.residual) {
 #pragma unroll
                 for (int p = 0; p < PASSES; ++p) __builtin_memcpy(&r[p], rp + (long long)(i * 16 + p * RPP) * a.ldr, 16);
             }
 #pragma unroll
-            for (int p = 0; p < PASSES; ++p) scale[p] = row_scale(a, m0 + i * 16 + p * RPP + r0);
+            for (int p = 0; p < PASSES; ++p) {
+                if constexpr (AHEAD) {
+                    r[p] = ahead.r[i][p];
+                    scale[p] = ahead.scale[i][p];
+                } else {
+                    scale[p] = row_scale(a, m0 + i * 16 + p * RPP + r0);
+                }
+            }
             stage(i);
 #pragma unroll
             for (int p = 0; p < PASSES; ++p) {
@@ -261,6 +297,12 @@ template <int DT, int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM 
     constexpr int READ_EVERY = M / (R + 1) > 0 ? M / (R + 1) : 1, LOAD_EVERY = M / L > 0 ? M / L : 1;  // MFMAs
     static_assert(M >= R && M >= L, "reads and loads fit behind the MFMAs");
 
+    const long long mw = m0 + wm * TM * 16;
+    const int nw = n0 + wn * TN * 16;
+    const auto ahead = [&] {  // in bf16 3136x512 -> 512 with a residual 6.2 -> 5.6 us, 5000x256 -> 256 4.8 -> 4.4; in fp32 it cost 0.3
+        if constexpr (BM == 64 && DT == SGPRS_BF16) return Ahead<DT, TM, TN>(a, mw, nw);
+        else return NotAhead();
+    }();
 #pragma unroll
     for (int i = 0; i < L; ++i) request(0, i);
 #pragma unroll
@@ -299,7 +341,7 @@ template <int DT, int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM 
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     static_assert(NW * StagedRows<DT, TN>::BYTES <= 2 * STAGE, "staging fits");
-    store_tile<DT, ACT, TM, TN>(a, acc, (int*)(smem + wave * StagedRows<DT, TN>::BYTES), m0 + wm * TM * 16, n0 + wn * TN * 16);
+    store_tile<DT, ACT, TM, TN>(a, acc, (int*)(smem + wave * StagedRows<DT, TN>::BYTES), mw, nw, ahead);
 #endif
 }
 
@@ -375,7 +417,7 @@ template <int DT, int ACT, int BM, int BN> __global__ __launch_bounds__(256, 2) 
     }
     __syncthreads();
     static_assert(4 * StagedRows<DT, TN>::BYTES <= 2 * STAGE, "staging fits");
-    store_tile<DT, ACT, TM, TN>(a, acc, (int*)(smem + wave * StagedRows<DT, TN>::BYTES), m0 + wm * TM * 16, n0 + wn * TN * 16);
+    store_tile<DT, ACT, TM, TN>(a, acc, (int*)(smem + wave * StagedRows<DT, TN>::BYTES), m0 + wm * TM * 16, n0 + wn * TN * 16, NotAhead());
 #endif
 }
 
@@ -399,7 +441,7 @@ template <int DT, int ACT> __global__ __launch_bounds__(256) void linear_i8_shor
             const u32x4_t x = load_chunk<1>(a.x + min(m0 + i * 16 + frow, a.m - 1ll) * a.ldx, live);
             acc[j][i] = mma(w, x, i32x4_t{0, 0, 0, 0});
         }
-    store_tile<DT, ACT, TM, TN>(a, acc, staged[wave], m0, n0);
+    store_tile<DT, ACT, TM, TN>(a, acc, staged[wave], m0, n0, NotAhead());
 #endif
 }
 
