@@ -574,14 +574,16 @@ size_t linear_i8_workspace_bytes(const sgprs_linear_i8_desc_t&, int) { return 0;
 // 256 / 128 / 64 square tiles, 64x64 / 32x32 / 16x16 with k split: 16384x4096 -> 4096 237 / 283 / 430 us, 12544x512 -> 2048
 // 33 / 30 / 39, 2048x1024 -> 1024 19 / 9.5 / 7.1 / 10.8, 256x4096 -> 4096 43 / 23 / 18 / 10.6 / 22, 64x4096 -> 4096 42 / 23 /
 // 17 / 9.9 / 7.3 / 17, 1x4096 -> 4096 39 / 21 / 16 / 8.8 / 6.2 / 5.7.
-static int plan_linear_i8(const sgprs_linear_i8_desc_t& d, int cus, bool direct)
+static int plan_linear_i8(const sgprs_linear_i8_desc_t& d, int cus, bool direct, bool residual)
 {
     if (d.k < 16) return kShort;
     const double kt = (d.k + 127) / 128;
-    // k_alone: of one tile with a CU to itself; k_shared, end: of each where CUs have several
-    struct Tile { int kernel, b; double k_alone, k_shared, end; };
-    static const Tile tiled[3] = {{kTile256, 256, 1.5, 1.5, 9}, {kTile128, 128, 0.63, 0.43, 2.6}, {kTile64, 64, 0.42, 0.2, 0.6}};
-    static const Tile staged[2] = {{kStaged128, 128, 1.6, 0.9, 1.5}, {kStaged64, 64, 0.9, 0.42, 0.9}};
+    // k_alone, end_alone: of one tile with a CU to itself, k_shared, end: of each where CUs have several.  A tile alone waits
+    // for its residual and twice the bytes of fp32; 4100x130 -> 520 in fp32 with a residual 128 / 64 square tiles 14.0 / 7.9 us.
+    struct Tile { int kernel, b; double k_alone, end_alone, k_shared, end; };
+    static const Tile tiled[3] = {{kTile256, 256, 1.0, 8, 1.5, 9}, {kTile128, 128, 0.54, 2.4, 0.43, 2.6}, {kTile64, 64, 0.42, 1.3, 0.2, 0.6}};
+    static const Tile staged[2] = {{kStaged128, 128, 1.6, 3, 0.9, 1.5}, {kStaged64, 64, 0.87, 1.4, 0.42, 0.9}};
+    const double wait = 1 + (d.dtype == SGPRS_F32 ? 0.5 : 0) + (residual ? 0.8 : 0);
     struct Split { int kernel, bm, bn; };
     static const Split split[7] = {{kSplit64x64, 64, 64}, {kSplit64x32, 64, 32}, {kSplit32x64, 32, 64}, {kSplit32x32, 32, 32}, {kSplit64x16, 64, 16}, {kSplit32x16, 32, 16}, {kSplit16x16, 16, 16}};
     auto tiles = [&](int bm, int bn) { return (double)((d.m + (long long)bm - 1) / bm) * ((d.n + bn - 1) / bn); };
@@ -594,13 +596,13 @@ static int plan_linear_i8(const sgprs_linear_i8_desc_t& d, int cus, bool direct)
     };
     for (const Tile& t : tiled) {
         const double share = tiles(t.b, t.b) / cus;
-        if (direct) offer(t.kernel, 2.6 + std::max(kt * t.k_alone + 0.5, (t.b == 256 ? std::ceil(share) : share) * (kt * t.k_shared + t.end)));
+        if (direct) offer(t.kernel, 2.6 + std::max(kt * t.k_alone + t.end_alone * wait, (t.b == 256 ? std::ceil(share) : share) * (kt * t.k_shared + t.end)));
     }
     for (const Tile& t : staged)
-        if (!direct) offer(t.kernel, 2.6 + std::max(kt * t.k_alone + 0.5, tiles(t.b, t.b) / cus * (kt * t.k_shared + t.end)));
+        if (!direct) offer(t.kernel, 2.6 + std::max(kt * t.k_alone + t.end_alone * wait, tiles(t.b, t.b) / cus * (kt * t.k_shared + t.end)));
     for (const Split& s : split)
         if (direct || s.kernel == kSplit64x64 || s.kernel == kSplit32x32 || s.kernel == kSplit16x16)
-            offer(s.kernel, 3 + std::ceil(tiles(s.bm, s.bn) / cus) * (direct ? 2.3 + (s.bm + s.bn) * kt * 128 / 105e3 : 2 + (s.bm + s.bn) * kt * 128 / 45e3));
+            offer(s.kernel, 3 + std::ceil(tiles(s.bm, s.bn) / cus) * (0.8 * (wait - 1) + (direct ? 2.3 + (s.bm + s.bn) * kt * 128 / 105e3 : 2 + (s.bm + s.bn) * kt * 128 / 45e3)));
     return best;
 }
 
@@ -681,7 +683,7 @@ int launch_linear_i8(const sgprs_linear_i8_desc_t& d, const int8_t* x, const flo
     const LinearI8Args a = {(const unsigned char*)x, (const unsigned char*)w, x_scales, w_scales, bias, (const unsigned char*)residual, (unsigned char*)y,
                             d.m, d.n, d.k, (int)d.ldx, (int)d.ldw, (int)d.ldr * es, (int)d.ldy * es, d.residual_first, 0, 0};
     const bool direct = (((uintptr_t)x | (uintptr_t)w | (unsigned)a.ldx | (unsigned)a.ldw | (unsigned)a.k) & 15) == 0;
-    const int kernel = plan_linear_i8(d, cus, direct);
+    const int kernel = plan_linear_i8(d, cus, direct, residual != nullptr);
     if (d.dtype == SGPRS_BF16)
         return direct ? launch_act<SGPRS_BF16, true>(a, d.act, kernel, stream) : launch_act<SGPRS_BF16, false>(a, d.act, kernel, stream);
     return direct ? launch_act<SGPRS_F32, true>(a, d.act, kernel, stream) : launch_act<SGPRS_F32, false>(a, d.act, kernel, stream);

@@ -245,6 +245,15 @@ def test_linear_shapes(pools, name, shape):
     run_linear(pools, name, m, n, k, act=i % 4, bias=i % 3 != 1, res=i % 2 == 1, first=(i // 2) % 2, seed=i)
 
 
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(4090, 4080, 1024), (12500, 500, 512), (12500, 517, 509), (1000, 1001, 2050), (250, 4096, 2048), (256, 2040, 4096), (120, 4096, 4096), (24, 4096, 4096),
+                                   (50, 4090, 4096), (40, 1000, 8192)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("res", [False, True], ids=["", "residual"])
+def test_linear_tiles_of_every_size(pools, name, shape, res):
+    m, n, k = shape
+    run_linear(pools, name, m, n, k, act=int(res), bias=not res, res=res, seed=m)
+
+
 @pytest.mark.parametrize("shape", [(1, 100, 512), (20, 64, 300), (40, 200, 130), (300, 130, 96), (1000, 1500, 200), (3000, 2100, 256)], ids=lambda s: "x".join(map(str, s)))
 @pytest.mark.parametrize("pads,lead", [((16, 0, 8, 8), 0), ((16, 32, 0, 0), 16), ((3, 0, 1, 5), 0), ((0, 1, 3, 0), 1), ((8, 4, 2, 6), 4), ((1, 1, 1, 1), 7)], ids=str)
 def test_linear_strides_and_alignment(pools, shape, pads, lead):
