@@ -369,7 +369,8 @@ int sgprs_attention(const sgprs_attention_desc_t *d, const void *q, const void *
  *   ->  sgprs_paged_append (k, v)  ->  sgprs_paged_attention (q)
  *   ->  sgprs_quantize_i8  ->  sgprs_linear_i8  ->  ...
  *
- * Strides, alignment, empty calls and overlaps are as for attention blocks.
+ * Strides, alignment, empty calls and overlaps are as for attention blocks; a
+ * workspace belongs to a call, or to a replay of a graph, until that has ended.
  * Statistics, sums and softmax are held in 32 bits or more; products of 8-bit
  * integers are summed exactly.
  *
@@ -439,13 +440,16 @@ int sgprs_linear_i8(const sgprs_linear_i8_desc_t *d, const int8_t *x, const floa
  * their values cannot be refused: a length beyond table_width * page_size (or
  * negative) counts as the nearest possible one, what would go to a page outside
  * 0 .. n_pages - 1 is not written, and what is read from there is unspecified, but nothing
- * outside the tensors is read or written. */
+ * outside the tensors is read or written.  They must not change while a call runs.
+ * UNSUPPORTED: more than 2^20 sequences, 65535 heads, 2^30 positions of a sequence, or
+ * 2^28 of (sequence, key head, 32 query heads of it) together. */
 
 /* The new keys and values of n_seqs sequences to their places in the cache: they
  * are the last ones of the kv_lens[s] positions that sequence s has with them.
  * Tokens offsets[s] .. offsets[s+1]-1 of k and v belong to sequence s (offsets
- * NULL: token s does, one for each).  A token whose position would be negative, as where kv_lens[s] is
- * 0, goes nowhere.  If a place is written twice, either may be there. */
+ * NULL: token s does, one for each).  A token whose position would be negative, as
+ * where kv_lens[s] is 0, goes nowhere.  If a place is written twice, each 16 bytes of
+ * it may come from either. */
 typedef struct {
     int n_seqs, total;              /* sequences, tokens in k and v */
     int kv_heads, head_dim;         /* head_dim a multiple of 8, up to 128 */

@@ -454,6 +454,46 @@ def test_attention_values_that_are_not_finite_where_they_are_seen(pools, name):
 
 
 @pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,dim", [(4, 64), (24, 128)])
+def test_attention_queries_and_keys_that_are_not_finite(pools, name, heads, dim):
+    """A NaN of a query stays in its head, one of a key in the heads that read it."""
+    kv, group = [200, 33, 700], heads // 2
+    q = (torch.randn(3, heads * dim, generator=gen(6)) * 1.5).to(DT[name][1])
+    clean = run_attention(pools, name, kv, heads, 2, dim, q=q, unseen=None, seed=5).view(3, heads, dim)
+    for at, value in ((0, NAN), (2, NAN), (2, INF)):
+        bad = q.clone()
+        bad.view(3, heads, dim)[at, 1, 3] = value
+        got = run_attention(pools, name, kv, heads, 2, dim, q=bad, unseen=None, seed=5).view(3, heads, dim)
+        assert bool(got[at, 1].isnan().all())
+        got[at, 1] = clean[at, 1]
+        assert torch.equal(bits(got), bits(clean)), (at, value)
+    c = Cache(name, kv, 16, 2, dim, seed=5)
+    c.to(c.k)[c.table[2, 20], 5, 1, 2] = NAN
+    got = run_attention(pools, name, kv, heads, 2, dim, q=q, cache=c, unseen=None, seed=5).view(3, heads, dim)
+    assert bool(got[2, group:].isnan().all())
+    got[2, group:] = clean[2, group:]
+    assert torch.equal(bits(got), bits(clean))
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("heads", [2, 6, 9])
+@pytest.mark.parametrize("first,last", [(0, 128), (0, 300), (128, 256), (40, 400), (0, 399)])
+def test_attention_scores_of_minus_infinity(pools, name, heads, first, last):
+    """Keys whose scores are -inf have no weight, as if they were not there, in tiles of nothing else too."""
+    kv, dim = [400, 100], 64
+    q = (torch.randn(2, heads * dim, generator=gen(6)) * 1.5).to(DT[name][1])
+    q.view(2, heads, dim)[:, :, 9] = 1.0
+    c = Cache(name, kv, 16, 1, dim, seed=7)
+    pos = torch.arange(first, last)
+    c.to(c.k)[c.table[0].long()[pos // 16], pos % 16, 0, 9] = -INF
+    got = run_attention(pools, name, kv, heads, 1, dim, q=q, cache=c, unseen=None, seed=7).view(2, heads, dim)
+    pos = torch.tensor([p for p in range(400) if not first <= p < last])
+    k, v = (t[c.table[0].long()[pos // 16], pos % 16] for t in c.host())
+    want, bound = block_ops_util.attention(q[:1].view(1, heads, dim), k, v, [1], [len(pos)], False, 0.0)
+    block_ops_util.assert_within(got[:1], want, bound, f"{name} without {first} to {last}")
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
 @pytest.mark.parametrize("scale", [-0.3, 1.0, 30.0, 1e-30])
 def test_attention_scales(pools, name, scale):
     run_attention(pools, name, [300, 40], 2, 2, 32, scale=scale)
@@ -594,6 +634,20 @@ def test_append_to_no_place(pools):
     run_append(pools, "f32", [20, 3], None, 2, 32, page=8, lens=[1 << 30, 0], table={(0, 3): lambda c: 0})
 
 
+def test_append_with_offsets_that_are_wrong(pools):
+    """Offsets that fall, are negative or pass the number of tokens: what is written comes from k and v, and nothing else changes."""
+    c = Cache("f32", [40, 40, 40, 40], 8, 2, 32, seed=2).to_gpu()
+    before = c.gk.clone(), c.gv.clone()
+    k, v = (torch.full((20, 64), t, device="cuda") for t in (5.0, 6.0))
+    for offsets in ([0, 12, 3, 9, 20], [-7, 2, 5, 9, 20], [0, 5, 9, 30, 2 ** 31 - 1], [7, 7, 7, 7, 7], [-2 ** 31, 2 ** 31 - 1, 0, -5, 3], [2 ** 31 - 1] * 5):
+        off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+        S.sgprs_paged_append(S.PagedAppendDesc(total=20, **c.dims), ptr(k), ptr(v), ptr(off), ptr(c.gtable), ptr(c.glens), ptr(c.gk), ptr(c.gv), pools(), 0)
+        pools().sync()
+        for now, was, new in ((c.gk, before[0], 5.0), (c.gv, before[1], 6.0)):
+            assert bool(((now == was) | (now == new)).all()), offsets
+
+
 # ---- calls ---------------------------------------------------------------------------------------
 def test_refusals_that_need_a_pool(pools):
     pool, p = pools(), torch.zeros(4096, device="cuda").data_ptr()
@@ -714,6 +768,46 @@ def test_a_step_in_a_graph_follows_lengths_that_grow(pools):
         block_ops_util.assert_within(rows, want, bound, f"step {i}")
         for s_, p in enumerate(lens):
             assert torch.equal(bits(hk_[cache.table[s_, (p - 1) // page], (p - 1) % page]), bits(got_rows[s_, heads * dim:heads * dim + kv].view(hk, dim)))
+
+
+def test_two_graphs_that_share_a_workspace(pools):
+    """Replayed in turn on one stream, with lengths that change between the replays."""
+    pool = pools()
+    kv = [900, 3000, 17, 0]
+    calls = []
+    for i, (name, heads, hk, dim) in enumerate((("bf16", 8, 2, 64), ("f32", 6, 2, 96))):
+        c = Cache(name, kv, 16, hk, dim, seed=i).to_gpu()
+        d = S.PagedAttentionDesc(heads=heads, **c.dims)
+        q = torch.randn(len(kv), heads * dim, generator=gen(i)).to(DT[name][1])
+        calls.append((c, d, q, q.cuda(), torch.empty_like(q, device="cuda"), S.sgprs_paged_attention_workspace(d, CUS)))
+    ws = torch.empty(max(t[5] for t in calls), dtype=torch.uint8, device="cuda")
+    stream, graphs = torch.cuda.ExternalStream(pool.stream(0)), []
+
+    def call(c, d, _, gq, o, need):
+        S.sgprs_paged_attention(d, ptr(gq), ptr(c.gk), ptr(c.gv), ptr(c.gtable), ptr(c.glens), ptr(o), ptr(ws), need, pool, 0)
+
+    torch.cuda.synchronize()
+    for t in calls:
+        call(*t)
+        pool.sync()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.stream(stream):
+            graphs[-1].capture_begin()
+            call(*t)
+            graphs[-1].capture_end()
+    for lens in (kv, [3, 2500, 17, 0], [0, 0, 0, 0], kv, [900, 1, 0, 0]):
+        for c, _, _, _, o, _ in calls:
+            c.glens.copy_(torch.tensor(lens, dtype=torch.int32))
+            o.fill_(NAN)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            for g in graphs:
+                g.replay()
+        torch.cuda.synchronize()
+        for c, d, q, _, o, _ in calls:
+            k, v = c.host()
+            want, bound = ref.paged_attention(q.view(len(kv), d.heads, d.head_dim), k, v, c.table, lens, 0, 0, 0.0)
+            block_ops_util.assert_within(o.view(len(kv), d.heads, d.head_dim), want, bound, f"{lens}")
 
 
 def test_two_partitions_at_once(pools):
