@@ -86,14 +86,20 @@ template <int DT, int ACT, int V> __device__ __forceinline__ u32x4_t finish(cons
 }
 
 // The same for a row and columns that may lie outside, and rows at any alignment.
-template <int DT, int ACT, int V> __device__ __forceinline__ void finish_row(const LinearI8Args& a, long long row, int col, const int* s, float x_scale, const Columns<V>& c)
+template <int V> __device__ __forceinline__ u32x4_t residual_at(const LinearI8Args& a, long long row, int col)
+{
+    constexpr int ES = 16 / V;
+    const bool live = a.residual && row < a.m && col < a.n;
+    return live ? load_chunk<ES>(a.residual + row * a.ldr + (long long)col * ES, min(V, a.n - col) * ES) : u32x4_t{0, 0, 0, 0};
+}
+template <int DT, int ACT, int V>
+__device__ __forceinline__ void finish_row(const LinearI8Args& a, long long row, int col, const int* s, float x_scale, const Columns<V>& c, u32x4_t r)
 {
     constexpr int ES = 16 / V;
     if (row >= a.m || col >= a.n) return;
-    const unsigned char* rp = a.residual + row * a.ldr + (long long)col * ES;
     unsigned char* yp = a.y + row * a.ldy + (long long)col * ES;
     const int live = min(V, a.n - col);
-    const u32x4_t out = finish<DT, ACT>(a, s, x_scale, c, a.residual ? load_chunk<ES>(rp, live * ES) : u32x4_t{0, 0, 0, 0});
+    const u32x4_t out = finish<DT, ACT>(a, s, x_scale, c, r);
     if (live == V) {
         __builtin_memcpy(yp, &out, 16);
     } else {
@@ -214,7 +220,7 @@ __device__ __forceinline__ void store_tile(const LinearI8Args& a, const i32x4_t 
                 int s[V];
                 staged(p, s);
                 const long long row = m0 + i * 16 + p * RPP + r0;
-                finish_row<DT, ACT>(a, row, col, s, row_scale(a, row), columns);
+                finish_row<DT, ACT>(a, row, col, s, row_scale(a, row), columns, residual_at<V>(a, row, col));
             }
             read();
         });
@@ -452,7 +458,7 @@ template <int DT, int ACT> __global__ __launch_bounds__(256) void linear_i8_shor
 // ---- few tiles: K split over the wavefronts of a workgroup ---------------------------------------
 // 16 TM x 16 TN outputs per workgroup; wavefront v takes k-tiles v, v + NW, ..., moves them into an LDS ring of its own and
 // meets the others at the end only, where the partial tiles are added.  Bound by the L2 -> CU path (about 105 GB/s a CU here)
-// and, for the fewest rows, the memory: 24x4096 -> 4096 in 6.5 us, 24x4096 -> 16384 in 13.2 (5.2 TB/s), 256x4096 -> 4096 in 10.6.
+// and, for the fewest rows, the memory: 24x4096 -> 4096 in 6.3 us, 24x4096 -> 16384 in 12.9 (5.2 TB/s), 256x4096 -> 4096 in 10.6.
 // (Fragments straight from memory to registers, without LDS: 7.9, 26 and 45 us: 64 bytes of a row at a time.)
 // Aligned rows by loads that write LDS directly; others (k >= 16) through registers, the next k-tile on its way.
 template <int DT, int ACT, int TM, int TN, int NW, int NS, bool DIRECT> __global__ __launch_bounds__(NW * 64, 1) void linear_i8_ksplit_kernel(const LinearI8Args a)
@@ -500,13 +506,17 @@ template <int DT, int ACT, int TM, int TN, int NW, int NS, bool DIRECT> __global
         for (int i = 0; i < TM; ++i) acc[j][i] = i32x4_t{0, 0, 0, 0};
     const int frow = lane & 15, fgrp = lane >> 4;
     const unsigned w_frag = ring + (unsigned)(frow * 128) + (unsigned)((fgrp ^ (frow & 7)) << 4), x_frag = w_frag + BN * 128;
+    // what this thread's first outputs need beside the sums (asked for behind the k loop: 24x4096 -> 16384 13.4 us for 12.9)
+    const int c0 = (int)threadIdx.x % LPR * V, r0 = (int)threadIdx.x / LPR;
+    const Columns<V> columns(a, n0 + c0);
+    const float scale0 = row_scale(a, m0 + r0);
+    const u32x4_t res0 = residual_at<V>(a, m0 + r0, n0 + c0);
     if constexpr (DIRECT) {
 #pragma unroll
         for (int s = 0; s < NS; ++s) request(wave + s * NW, s);
     } else {
         request(wave, 0);
     }
-    const int c0 = (int)threadIdx.x % LPR * V;
     int slot = 0;
     for (int t = wave; t < tiles; t += NW) {
         if constexpr (DIRECT) {
@@ -546,7 +556,6 @@ template <int DT, int ACT, int TM, int TN, int NW, int NS, bool DIRECT> __global
                 for (int i = 0; i < TM; ++i) acc[j][i] = mma(wf[h][j], xf[h][i], acc[j][i]);
         slot = slot + 1 == NS ? 0 : slot + 1;
     }
-    const Columns<V> columns(a, n0 + c0);
     __builtin_amdgcn_s_waitcnt(0);  // requests past the end write zeros into the ring
     int* mine = (int*)(smem + ring);
 #pragma unroll
@@ -555,13 +564,13 @@ template <int DT, int ACT, int TM, int TN, int NW, int NS, bool DIRECT> __global
         for (int j = 0; j < TN; ++j) *(i32x4_t*)(mine + (i * 16 + frow) * SROW + j * 16 + fgrp * 4) = acc[j][i];
     __syncthreads();
     static_assert(NW * 64 % LPR == 0, "a thread keeps its columns");
-    for (int r = (int)threadIdx.x / LPR; r < BM; r += NW * 64 / LPR) {
+    for (int r = r0; r < BM; r += NW * 64 / LPR) {
         i32x4_t total[V / 4] = {};
 #pragma unroll
         for (int v = 0; v < NW; ++v)
 #pragma unroll
             for (int e = 0; e < V / 4; ++e) total[e] += *(const i32x4_t*)((const int*)(smem + v * NS * STAGE) + r * SROW + c0 + 4 * e);
-        finish_row<DT, ACT>(a, m0 + r, n0 + c0, (const int*)total, row_scale(a, m0 + r), columns);
+        finish_row<DT, ACT>(a, m0 + r, n0 + c0, (const int*)total, r == r0 ? scale0 : row_scale(a, m0 + r), columns, r == r0 ? res0 : residual_at<V>(a, m0 + r, n0 + c0));
     }
 #endif
 }
