@@ -770,6 +770,90 @@ def test_a_step_in_a_graph_follows_lengths_that_grow(pools):
             assert torch.equal(bits(hk_[cache.table[s_, (p - 1) // page], (p - 1) % page]), bits(got_rows[s_, heads * dim:heads * dim + kv].view(hk, dim)))
 
 
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_a_layer_of_a_decoding_step(pools, name):
+    """All of the operators in a row, as a layer uses them: weights to integers once, then norm, q / k / v, append, attention,
+    output product on top of the residual, norm with its addition, and the two products behind it; each against the
+    definition of what the one before it gave."""
+    dt, tdt = DT[name]
+    pool, g = pools(), gen(9)
+    n, c, heads, hk, dim, wide = 6, 320, 4, 2, 40, 700
+    kv = hk * dim
+    cache = Cache(name, [5, 1, 260, 33, 700, 64], 16, hk, dim, seed=2).to_gpu()
+    lens = cache.lens.tolist()
+
+    def empty(*shape, dtype=tdt):
+        return torch.zeros(*shape, dtype=dtype, device="cuda")
+
+    def weights(rows, k):
+        w = (torch.randn(rows, k, generator=g) / math.sqrt(k)).to(tdt)
+        gw, q, sc = w.cuda(), empty(rows, k, dtype=torch.int8), empty(rows, dtype=torch.float32)
+        torch.cuda.synchronize()
+        S.sgprs_quantize_i8(S.QuantizeDesc(m=rows, c=k, dtype=dt), ptr(gw), ptr(q), ptr(sc), pool, 0)
+        pool.sync()
+        want, ws = ref.quantize(w)
+        same(q, want, "weights")
+        return q, sc
+
+    def product(x, sx, w, act=0, res=None, on=None):
+        q, sw = w
+        rows = q.shape[0]
+        y = on if on is not None else empty(n, rows)
+        rh = res.cpu() if res is not None else None
+        d = S.LinearI8Desc(m=n, n=rows, k=q.shape[1], dtype=dt, act=act)
+        torch.cuda.synchronize()
+        S.sgprs_linear_i8(d, ptr(x), ptr(sx), ptr(q), ptr(sw), None, ptr(res) if res is not None else None, ptr(y), None, 0, pool, 0)
+        pool.sync()
+        want, bound = ref.linear_i8(x.cpu(), sx.cpu(), q.cpu(), sw.cpu(), None, rh, act, 0, tdt)
+        block_ops_util.assert_within(y, want, bound, f"product to {rows}")
+        return y
+
+    def norm(x, res, gamma, sum_on):
+        q, sc, xh, rh = empty(n, c, dtype=torch.int8), empty(n, dtype=torch.float32), x.cpu(), res.cpu() if res is not None else None
+        torch.cuda.synchronize()
+        S.sgprs_rms_norm(S.RmsNormDesc(m=n, c=c, dtype=dt, out_dtype=S.SGPRS_I8, eps=1e-6), ptr(x), ptr(res) if res is not None else None, ptr(gamma),
+                         ptr(sum_on) if sum_on is not None else None, ptr(q), ptr(sc), pool, 0)
+        pool.sync()
+        h, want, _ = ref.rms_norm(xh, rh, gamma.cpu(), 1e-6, True)
+        same(q, want, "norm")
+        assert sum_on is None or torch.equal(bits(sum_on.cpu()), bits(h))
+        return q, sc
+
+    w_qkv, w_o, w_up, w_down = weights(heads * dim + 2 * kv, c), weights(c, heads * dim), weights(wide, c), weights(c, wide)
+    gamma = [(torch.rand(c, generator=g) + 0.5).cuda() for _ in range(3)]
+    x = torch.randn(n, c, generator=g).to(tdt).cuda()
+    rows = product(*norm(x, None, gamma[0], None), w_qkv)
+    es, ld = rows.element_size(), rows.shape[1]
+    S.sgprs_paged_append(S.PagedAppendDesc(total=n, ldk=ld, ldv=ld, **cache.dims), ptr(rows) + heads * dim * es, ptr(rows) + (heads * dim + kv) * es, None, ptr(cache.gtable),
+                         ptr(cache.glens), ptr(cache.gk), ptr(cache.gv), pool, 0)
+    d = S.PagedAttentionDesc(heads=heads, ldq=ld, **cache.dims)
+    need, o = S.sgprs_paged_attention_workspace(d, CUS), empty(n, heads * dim)
+    ws = empty(need, dtype=torch.uint8)
+    torch.cuda.synchronize()
+    S.sgprs_paged_attention(d, ptr(rows), ptr(cache.gk), ptr(cache.gv), ptr(cache.gtable), ptr(cache.glens), ptr(o), ptr(ws), need, pool, 0)
+    pool.sync()
+    rh = rows.cpu()
+    k, v = ref.paged_append(*(t.reshape(n, hk, dim) for t in rh[:, heads * dim:].split(kv, 1)), None, cache.table, lens, *cache.host())
+    cache.k, cache.v = cache.gk.cpu(), cache.gv.cpu()
+    for a, b in zip(cache.host(), (k, v)):
+        assert torch.equal(bits(a), bits(b))
+    want, bound = ref.paged_attention(rh[:, :heads * dim].reshape(n, heads, dim), k, v, cache.table, lens, 0, 0, 0.0)
+    block_ops_util.assert_within(o.view(n, heads, dim), want, bound, "attention")
+    q8, sc = empty(n, heads * dim, dtype=torch.int8), empty(n, dtype=torch.float32)
+    torch.cuda.synchronize()
+    S.sgprs_quantize_i8(S.QuantizeDesc(m=n, c=heads * dim, dtype=dt), ptr(o), ptr(q8), ptr(sc), pool, 0)
+    pool.sync()
+    same(q8, ref.quantize(o.cpu())[0], "attention's rows")
+    y = product(q8, sc, w_o)
+    up = product(*norm(y, x, gamma[1], x), w_up, act=3)
+    q8, sc = empty(n, wide, dtype=torch.int8), empty(n, dtype=torch.float32)
+    torch.cuda.synchronize()
+    S.sgprs_quantize_i8(S.QuantizeDesc(m=n, c=wide, dtype=dt), ptr(up), ptr(q8), ptr(sc), pool, 0)
+    pool.sync()
+    product(q8, sc, w_down, res=x, on=x)
+    norm(x, None, gamma[2], None)
+
+
 def test_two_graphs_that_share_a_workspace(pools):
     """Replayed in turn on one stream, with lengths that change between the replays."""
     pool = pools()
