@@ -249,12 +249,14 @@ template <int N, int M> __device__ __forceinline__ void settle(i32x4_t (&acc)[N]
 }
 
 // ---- tiles shared by a workgroup: aligned rows --------------------------------------------------
-// BM x BN outputs, 2 x 2 wavefronts; two k-tiles in LDS, filled by loads that write it directly.  The barrier of a k-tile
+// BM x BN outputs, 2 x 2 wavefronts; two k-tiles (or NS) in LDS, filled by loads that write it directly.  The barrier of a k-tile
 // stands between its two halves: before it the second half's fragments have been read, so that its MFMAs follow the barrier
 // at once while the next k-tile's first fragments are read and the one after that is requested into the buffer just left.
+// NS k-tiles in LDS: four where few tiles leave it free, 1024x4096 -> 4096 by 128x128 tiles 26 -> 22 us, 256x4096 -> 4096 by
+// 64x64 18 -> 10.6; where several workgroups share a CU two are faster (2048x4096 -> 4096 35 for 42).
 // 16384x4096 -> 4096 in 240 to 255 us, by card (2.2 to 2.3 PFLOP/s; the library's product of integers alone 259): bound by
 // the MFMAs and the clock under them.  32x32x32 MFMAs took 255 for 237, a ring of four half k-tiles 258 for 255.
-template <int DT, int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM * BN >= 256 * 128 ? 1 : 2) void linear_i8_tile_kernel(const LinearI8Args a)
+template <int DT, int ACT, int BM, int BN, int NS> __global__ __launch_bounds__(256, BM * BN >= 256 * 128 ? 1 : 2) void linear_i8_tile_kernel(const LinearI8Args a)
 {
 #if __HIP_DEVICE_COMPILE__
     constexpr int WM = 2, WN = 2, NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
@@ -277,7 +279,7 @@ template <int DT, int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM 
     // load i of k-tile t; past the last k-tile everything lies outside
     auto request = [&](int t, int i) {
         const bool live = t * 128 + chunk * 16 < a.k;
-        unsigned char* st = smem + (t & 1) * STAGE;
+        unsigned char* st = smem + (t & (NS - 1)) * STAGE;
         if (i < LA)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(x_rs, (lds_ptr_t)(st + (wave * LA + i) * 1024), 16, live ? x_off + (unsigned)(i * 8 * a.ldx) : kOutside,
                                                      t * 128, 0, 0);
@@ -297,13 +299,14 @@ template <int DT, int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM 
     u32x4_t xf[2][TM], wf[2][TN];
     // fragment r of half h of k-tile t
     auto read_fragment = [&](int t, int h, int r) {
-        const unsigned base = (unsigned)((t & 1) * STAGE);
+        const unsigned base = (unsigned)((t & (NS - 1)) * STAGE);
         if (r < TN) wf[h][r] = lds_read((w_frag + base + r * 2048) ^ (h << 6));
         else xf[h][r - TN] = lds_read((x_frag + base + (r - TN) * 2048) ^ (h << 6));
     };
     constexpr int R = TM + TN, M = TM * TN;
     constexpr int READ_EVERY = M / (R + 1) > 0 ? M / (R + 1) : 1, LOAD_EVERY = M / L > 0 ? M / L : 1;  // MFMAs
     static_assert(M >= R && M >= L, "reads and loads fit behind the MFMAs");
+    static_assert((NS & (NS - 1)) == 0 && (NS - 1) * L <= 63, "slots by masks, vmcnt range");
 
     const long long mw = m0 + wm * TM * 16;
     const int nw = n0 + wn * TN * 16;
@@ -312,10 +315,11 @@ template <int DT, int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM 
         else return NotAhead();
     }();
 #pragma unroll
-    for (int i = 0; i < L; ++i) request(0, i);
+    for (int s = 0; s < NS; ++s)
 #pragma unroll
-    for (int i = 0; i < L; ++i) request(1, i);
-    __builtin_amdgcn_s_waitcnt((L & 15) | ((L >> 4) << 14) | 0x0F70);  // the first k-tile has landed
+        for (int i = 0; i < L; ++i) request(s, i);
+    constexpr int BEHIND = (NS - 1) * L, NEXT = (NS - 2) * L;  // requests behind the first k-tile, and behind the next one
+    __builtin_amdgcn_s_waitcnt((BEHIND & 15) | ((BEHIND >> 4) << 14) | 0x0F70);  // the first k-tile has landed
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -331,7 +335,7 @@ template <int DT, int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM 
                 if (at % READ_EVERY == 0 && at / READ_EVERY < R) read_fragment(t, 1, at / READ_EVERY);
                 __builtin_amdgcn_sched_barrier(0);
             }
-        __builtin_amdgcn_s_waitcnt(0x0070);  // the next k-tile has landed, the fragments are read
+        __builtin_amdgcn_s_waitcnt((NEXT & 15) | ((NEXT >> 4) << 14) | 0x0070);  // the next k-tile has landed, the fragments are read
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -340,7 +344,7 @@ template <int DT, int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM 
             for (int i = 0; i < TM; ++i) {
                 const int at = j * TM + i;
                 mma_tied(wf[1][j], xf[1][i], acc[j][i]);
-                if (at % LOAD_EVERY == 0 && at / LOAD_EVERY < L) request(t + 2, at / LOAD_EVERY);
+                if (at % LOAD_EVERY == 0 && at / LOAD_EVERY < L) request(t + NS, at / LOAD_EVERY);
                 if (at % READ_EVERY == 0 && at / READ_EVERY < R) read_fragment(t + 1, 0, at / READ_EVERY);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -348,7 +352,7 @@ template <int DT, int ACT, int BM, int BN> __global__ __launch_bounds__(256, BM 
     settle(acc);
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    static_assert(NW * StagedRows<DT, TN>::BYTES <= 2 * STAGE, "staging fits");
+    static_assert(NW * StagedRows<DT, TN>::BYTES <= NS * STAGE, "staging fits");
     store_tile<DT, ACT, TM, TN>(a, acc, (int*)(smem + wave * StagedRows<DT, TN>::BYTES), mw, nw, ahead);
 #endif
 }
@@ -576,7 +580,7 @@ template <int DT, int ACT, int TM, int TN, int NW, int NS, bool DIRECT> __global
 }
 
 // ---- plans -------------------------------------------------------------------------------------
-enum LinearI8Kernel { kTile256, kTile128, kTile64, kStaged128, kStaged64, kSplit16x16, kSplit32x16, kSplit64x16, kSplit32x32, kSplit64x32, kSplit32x64, kSplit64x64, kShort };
+enum LinearI8Kernel { kTile256, kTile128, kTile64, kDeep128, kDeep64, kStaged128, kStaged64, kSplit16x16, kSplit32x16, kSplit64x16, kSplit32x32, kSplit64x32, kSplit32x64, kSplit64x64, kShort };
 
 // Integers are summed exactly in any order, but no kernel splits k over workgroups: with a join in a second launch 128x4096
 // -> 4096 took 17 us, where the wavefronts of a workgroup split it in 8.5.
@@ -585,8 +589,8 @@ size_t linear_i8_workspace_bytes(const sgprs_linear_i8_desc_t&, int) { return 0;
 // direct: operands whose rows are whole aligned chunks.  The kernel with the least estimate, in us, fitted to measurements on
 // 256 CUs (three sets of inputs in turn): what a launch takes, and what the busiest CU's tiles do, by their k-tiles.
 // 256 / 128 / 64 square tiles, 64x64 / 32x32 / 16x16 with k split: 16384x4096 -> 4096 237 / 283 / 430 us, 12544x512 -> 2048
-// 33 / 30 / 39, 2048x1024 -> 1024 19 / 9.5 / 7.1 / 10.8, 256x4096 -> 4096 43 / 23 / 18 / 10.6 / 22, 64x4096 -> 4096 42 / 23 /
-// 17 / 9.9 / 7.3 / 17, 1x4096 -> 4096 39 / 21 / 16 / 8.8 / 6.2 / 5.7.
+// 33 / 30 / 39, 2048x1024 -> 1024 19 / 9.5 / 7.1 / 10.8, 256x4096 -> 4096 43 / 23 (17 with four k-tiles) / 18 (10.6) / 10.6 / 22, 64x4096 ->
+// 4096 42 / 23 / 17 / 9.9 / 7.3 / 17, 1x4096 -> 4096 39 / 21 / 16 / 8.8 / 6.2 / 5.7.
 static int plan_linear_i8(const sgprs_linear_i8_desc_t& d, int cus, bool direct, bool residual)
 {
     if (d.k < 16) return kShort;
@@ -594,7 +598,7 @@ static int plan_linear_i8(const sgprs_linear_i8_desc_t& d, int cus, bool direct,
     // k_alone, end_alone: of one tile with a CU to itself, k_shared, end: of each where CUs have several.  A tile alone waits
     // for its residual and twice the bytes of fp32; 4100x130 -> 520 in fp32 with a residual 128 / 64 square tiles 14.0 / 7.9 us.
     struct Tile { int kernel, b; double k_alone, end_alone, k_shared, end; };
-    static const Tile tiled[3] = {{kTile256, 256, 1.0, 8, 1.5, 9}, {kTile128, 128, 0.54, 2.4, 0.43, 2.6}, {kTile64, 64, 0.42, 1.3, 0.2, 0.6}};
+    static const Tile tiled[3] = {{kTile256, 256, 1.0, 8, 1.5, 9}, {kTile128, 128, 0.54, 2.9, 0.43, 2.6}, {kTile64, 64, 0.42, 1.3, 0.2, 0.6}};
     static const Tile staged[2] = {{kStaged128, 128, 1.6, 3, 0.9, 1.5}, {kStaged64, 64, 0.87, 1.4, 0.42, 0.9}};
     const double wait = 1 + (d.dtype == SGPRS_F32 ? 0.5 : 0) + (residual ? 0.8 : 0);
     struct Split { int kernel, bm, bn; };
@@ -611,6 +615,10 @@ static int plan_linear_i8(const sgprs_linear_i8_desc_t& d, int cus, bool direct,
         const double share = tiles(t.b, t.b) / cus;
         if (direct) offer(t.kernel, 2.6 + std::max(kt * t.k_alone + t.end_alone * wait, (t.b == 256 ? std::ceil(share) : share) * (kt * t.k_shared + t.end)));
     }
+    // four k-tiles in LDS instead of two, for a workgroup (128) or two (64) on a CU: alone, a k-tile is a round trip
+    const double on128 = tiles(128, 128) / cus, on64 = std::ceil(tiles(64, 64) / cus);
+    if (direct && kt > 4 && on128 <= 1) offer(kDeep128, 2.6 + kt * (0.34 + 0.18 * on128) + 3 * wait);
+    if (direct && kt > 4 && on64 <= 2) offer(kDeep64, 2.6 + kt * 0.195 * on64 + 1.6 * wait);
     for (const Tile& t : staged)
         if (!direct) offer(t.kernel, 2.6 + std::max(kt * t.k_alone + t.end_alone * wait, tiles(t.b, t.b) / cus * (kt * t.k_shared + t.end)));
     for (const Split& s : split)
@@ -639,9 +647,9 @@ static LinearI8Args tiled(LinearI8Args a, int bm, int bn)
     return a;
 }
 
-template <int DT, int ACT, int BM, int BN> static int launch_tile(const LinearI8Args& a, hipStream_t stream)
+template <int DT, int ACT, int BM, int BN, int NS> static int launch_tile(const LinearI8Args& a, hipStream_t stream)
 {
-    return launch_sized<linear_i8_tile_kernel<DT, ACT, BM, BN>>(2 * (BM + BN) * 128, tiled(a, BM, BN), 256, stream);
+    return launch_sized<linear_i8_tile_kernel<DT, ACT, BM, BN, NS>>(NS * (BM + BN) * 128, tiled(a, BM, BN), 256, stream);
 }
 template <int DT, int ACT, int BM, int BN> static int launch_staged(const LinearI8Args& a, hipStream_t stream)
 {
@@ -657,9 +665,11 @@ template <int DT, int ACT, bool DIRECT> static int launch_planned(const LinearI8
     if (kernel == kShort) return launch_sized<linear_i8_short_kernel<DT, ACT>>(0, tiled(a, 64, 64), 256, stream);
     if constexpr (DIRECT) {
         switch (kernel) {
-        case kTile256: return launch_tile<DT, ACT, 256, 256>(a, stream);
-        case kTile128: return launch_tile<DT, ACT, 128, 128>(a, stream);
-        case kTile64: return launch_tile<DT, ACT, 64, 64>(a, stream);
+        case kTile256: return launch_tile<DT, ACT, 256, 256, 2>(a, stream);
+        case kTile128: return launch_tile<DT, ACT, 128, 128, 2>(a, stream);
+        case kTile64: return launch_tile<DT, ACT, 64, 64, 2>(a, stream);
+        case kDeep128: return launch_tile<DT, ACT, 128, 128, 4>(a, stream);
+        case kDeep64: return launch_tile<DT, ACT, 64, 64, 4>(a, stream);
         case kSplit32x16: return launch_ksplit<DT, ACT, true, 2, 1, 8, 3>(a, stream);
         case kSplit64x16: return launch_ksplit<DT, ACT, true, 4, 1, 4, 3>(a, stream);
         case kSplit64x32: return launch_ksplit<DT, ACT, true, 4, 2, 4, 3>(a, stream);

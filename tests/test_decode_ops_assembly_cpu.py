@@ -51,7 +51,7 @@ def test_products_of_integers(tmp_path):
         text, tiles = text.replace("v_mfma_i32_16x16x64_i8", "v_mfma_f32_16x16x32_bf16"), tiles + 1
         b = int(re.search(r"ELi(\d+)ELi\1E", name)[1])
         assert settled_operands(text) == check(text) == 2 * (b // 32) ** 2, name  # two halves of a k-tile, 2 x 2 wavefronts
-    assert tiles == 3 * 4 * 2  # sizes, activations, types
+    assert tiles == 5 * 4 * 2  # sizes and depths, activations, types
 
 
 def test_paged_attention(tmp_path):
