@@ -361,8 +361,9 @@ template <int DT, int ACT, int BM, int BN, int NS> __global__ __launch_bounds__(
 // BM x BN outputs, 2 x 2 wavefronts; the next k-tile is on its way to registers while this one, in one of two LDS buffers, is
 // multiplied.  k >= 16: loads have no branch; a chunk that reaches past the end of its row is taken from the row's
 // last 16 bytes and shifted when it is stored, rows past the end repeat the last one.
-// 3137x517 -> 509 in fp32 in 8 us, with a residual 9.5: few k-tiles, each a round trip to memory.  Two k-tiles on their way took
-// 8.6 for 7.5, residuals and scales asked for before the k loop 8.5 for 7.9.
+// Few tiles are 32 rows high: 700x700 -> 701 in bf16 5.9 us, by 64x64 tiles 7.3, 1000x1000 -> 500 7.2 for 8.2.
+// 3137x517 -> 509 in fp32 in 8 us, with a residual 9.1 (by 64x64 tiles 9.8): few k-tiles, each a round trip to memory.  Two
+// k-tiles on their way took 8.6 for 7.5, residuals and scales asked for before the k loop 8.5 for 7.9.
 template <int DT, int ACT, int BM, int BN> __global__ __launch_bounds__(256, 2) void linear_i8_staged_kernel(const LinearI8Args a)
 {
 #if __HIP_DEVICE_COMPILE__
@@ -580,7 +581,7 @@ template <int DT, int ACT, int TM, int TN, int NW, int NS, bool DIRECT> __global
 }
 
 // ---- plans -------------------------------------------------------------------------------------
-enum LinearI8Kernel { kTile256, kTile128, kTile64, kDeep128, kDeep64, kStaged128, kStaged64, kSplit16x16, kSplit32x16, kSplit64x16, kSplit32x32, kSplit64x32, kSplit32x64, kSplit64x64, kShort };
+enum LinearI8Kernel { kTile256, kTile128, kTile64, kDeep128, kDeep64, kStaged128, kStaged64, kStaged32, kSplit16x16, kSplit32x16, kSplit64x16, kSplit32x32, kSplit64x32, kSplit32x64, kSplit64x64, kShort };
 
 // Integers are summed exactly in any order, but no kernel splits k over workgroups: with a join in a second launch 128x4096
 // -> 4096 took 17 us, where the wavefronts of a workgroup split it in 8.5.
@@ -597,9 +598,9 @@ static int plan_linear_i8(const sgprs_linear_i8_desc_t& d, int cus, bool direct,
     const double kt = (d.k + 127) / 128;
     // k_alone, end_alone: of one tile with a CU to itself, k_shared, end: of each where CUs have several.  A tile alone waits
     // for its residual and twice the bytes of fp32; 4100x130 -> 520 in fp32 with a residual 128 / 64 square tiles 14.0 / 7.9 us.
-    struct Tile { int kernel, b; double k_alone, end_alone, k_shared, end; };
-    static const Tile tiled[3] = {{kTile256, 256, 1.0, 8, 1.5, 9}, {kTile128, 128, 0.54, 2.9, 0.43, 2.6}, {kTile64, 64, 0.42, 1.3, 0.2, 0.6}};
-    static const Tile staged[2] = {{kStaged128, 128, 1.6, 3, 0.9, 1.5}, {kStaged64, 64, 0.87, 1.4, 0.42, 0.9}};
+    struct Tile { int kernel, b, bn; double k_alone, end_alone, k_shared, end; };
+    static const Tile tiled[3] = {{kTile256, 256, 256, 1.0, 8, 1.5, 9}, {kTile128, 128, 128, 0.54, 2.9, 0.43, 2.6}, {kTile64, 64, 64, 0.42, 1.3, 0.2, 0.6}};
+    static const Tile staged[3] = {{kStaged128, 128, 128, 1.6, 3, 0.9, 1.5}, {kStaged64, 64, 64, 0.87, 1.4, 0.42, 0.9}, {kStaged32, 32, 64, 0.5, 0.6, 0.35, 0.45}};
     const double wait = 1 + (d.dtype == SGPRS_F32 ? 0.5 : 0) + (residual ? 0.8 : 0);
     struct Split { int kernel, bm, bn; };
     static const Split split[7] = {{kSplit64x64, 64, 64}, {kSplit64x32, 64, 32}, {kSplit32x64, 32, 64}, {kSplit32x32, 32, 32}, {kSplit64x16, 64, 16}, {kSplit32x16, 32, 16}, {kSplit16x16, 16, 16}};
@@ -612,7 +613,7 @@ static int plan_linear_i8(const sgprs_linear_i8_desc_t& d, int cus, bool direct,
         best = kernel;
     };
     for (const Tile& t : tiled) {
-        const double share = tiles(t.b, t.b) / cus;
+        const double share = tiles(t.b, t.bn) / cus;
         if (direct) offer(t.kernel, 2.6 + std::max(kt * t.k_alone + t.end_alone * wait, (t.b == 256 ? std::ceil(share) : share) * (kt * t.k_shared + t.end)));
     }
     // four k-tiles in LDS instead of two, for a workgroup (128) or two (64) on a CU: alone, a k-tile is a round trip
@@ -620,10 +621,10 @@ static int plan_linear_i8(const sgprs_linear_i8_desc_t& d, int cus, bool direct,
     if (direct && kt > 4 && on128 <= 1) offer(kDeep128, 2.6 + kt * (0.34 + 0.18 * on128) + 3 * wait);
     if (direct && kt > 4 && on64 <= 2) offer(kDeep64, 2.6 + kt * 0.195 * on64 + 1.6 * wait);
     for (const Tile& t : staged)
-        if (!direct) offer(t.kernel, 2.6 + std::max(kt * t.k_alone + t.end_alone * wait, tiles(t.b, t.b) / cus * (kt * t.k_shared + t.end)));
+        if (!direct) offer(t.kernel, 2.6 + std::max(kt * t.k_alone + t.end_alone * wait, tiles(t.b, t.bn) / cus * (kt * t.k_shared + t.end)));
     for (const Split& s : split)
         if (direct || s.kernel == kSplit64x64 || s.kernel == kSplit32x32 || s.kernel == kSplit16x16)
-            offer(s.kernel, 3 + std::ceil(tiles(s.bm, s.bn) / cus) * (0.8 * (wait - 1) + (direct ? 2.3 + (s.bm + s.bn) * kt * 128 / 105e3 : 2 + (s.bm + s.bn) * kt * 128 / 45e3)));
+            offer(s.kernel, 3 + std::ceil(tiles(s.bm, s.bn) / cus) * (0.8 * (wait - 1) + (direct ? 2.3 + (s.bm + s.bn) * kt * 128 / 105e3 : 0.2 + (s.bm + s.bn) / 53. + (s.bm + s.bn) * kt * 128 / 45e3)));
     return best;
 }
 
@@ -679,6 +680,7 @@ template <int DT, int ACT, bool DIRECT> static int launch_planned(const LinearI8
         switch (kernel) {
         case kStaged128: return launch_staged<DT, ACT, 128, 128>(a, stream);
         case kStaged64: return launch_staged<DT, ACT, 64, 64>(a, stream);
+        case kStaged32: return launch_staged<DT, ACT, 32, 64>(a, stream);
         }
     }
     switch (kernel) {

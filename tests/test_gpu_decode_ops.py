@@ -248,7 +248,8 @@ def test_linear_shapes(pools, name, shape):
 @pytest.mark.parametrize("name", ["f32", "bf16"])
 @pytest.mark.parametrize("shape", [(4090, 4080, 1024), (12500, 500, 512), (12500, 517, 509), (1000, 1001, 2050), (250, 4096, 2048), (256, 2040, 4096), (120, 4096, 4096), (24, 4096, 4096),
                                    (50, 4090, 4096), (40, 1000, 8192),
-                                   (1000, 4096, 2048), (700, 2040, 1536), (1000, 1024, 648), (500, 4096, 1024)], ids=lambda s: "x".join(map(str, s)))
+                                   (1000, 4096, 2048), (700, 2040, 1536), (1000, 1024, 648), (500, 4096, 1024),
+                                   (700, 701, 700), (1500, 300, 300), (2100, 517, 131)], ids=lambda s: "x".join(map(str, s)))
 @pytest.mark.parametrize("res", [False, True], ids=["", "residual"])
 def test_linear_tiles_of_every_size(pools, name, shape, res):
     m, n, k = shape
