@@ -471,7 +471,8 @@ int sgprs_paged_append(const sgprs_paged_append_desc_t *d, const void *k, const 
  * over positions j < kv_lens[s] of the sequence (its own key among them, appended
  * before); with a window, over the last `window` of them and the first `sinks`.
  * A sequence without a position gets zeros; positions that are not seen are not
- * read.  bf16 rounds as sgprs_attention does. */
+ * read.  In bf16 a weight is two bf16 parts for its product with v, off by 2^-15 of it,
+ * so that a result is rounded once (sgprs_attention's weights are one part). */
 typedef struct {
     int n_seqs;
     int heads, kv_heads, head_dim;  /* heads % kv_heads == 0; head_dim a multiple of 8, up to 128 */

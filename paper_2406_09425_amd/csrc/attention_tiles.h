@@ -171,15 +171,26 @@ __device__ __forceinline__ void add_values(f32x16_t* o, const float* p, unsigned
 
 // The same for bf16 with all of a block's fragments read at once.  The reads are inline assembly, waited for inside it: before
 // the builtins' the compiler waits for every load that writes LDS, the next tile's too.
+//
+// Weights are two bf16 parts: the bits that fit, and what is left, rounded, so that they are off by 2^-15 of them and a result
+// by little more than its own rounding.  The kernel that calls this is bound by the memory: 16 caches of 1 to 32768 tokens
+// 60.5 us for 60.2 with rounded weights, 128 of 300 37.6 for 36.9.  Where v is infinite 0 * v or a
+// negative part would make a NaN of it, so the first part is cut off, not rounded, and 2^-20 of the weight is added to the
+// second, which is then above zero wherever the weight is.
 template <int HD> __device__ __forceinline__ void add_values_at_once(f32x16_t* o, const float* p, unsigned v_base)
 {
     typedef KvTile<SGPRS_BF16, HD> Tile;
     constexpr int DB = HD / 32;
-    u32x4_t w[2];
+    u32x4_t w[2], rest[2];
+    auto left = [](float z) { return __builtin_fmaf(z, 1.f + 0x1p-20f, -__uint_as_float(__float_as_uint(z) & 0xffff0000u)); };
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[u][e] = pack_bf16x2_relu(p[8 * u + 2 * e], p[8 * u + 2 * e + 1], kNoReluFloor);
+        for (int e = 0; e < 4; ++e) {
+            const float even = p[8 * u + 2 * e], odd = p[8 * u + 2 * e + 1];
+            w[u][e] = __builtin_amdgcn_perm(__float_as_uint(odd), __float_as_uint(even), 0x07060302u);
+            rest[u][e] = pack_bf16x2_relu(left(even), left(odd), kNoReluFloor);
+        }
 #pragma unroll
     for (int d0 = 0; d0 < DB; d0 += 2) {
         constexpr int N = DB > 1 ? 2 : 1;
@@ -208,6 +219,7 @@ template <int HD> __device__ __forceinline__ void add_values_at_once(f32x16_t* o
                 if (d0 + d >= DB) continue;
                 const u32x4_t v = {f[d][u][0][0], f[d][u][0][1], f[d][u][1][0], f[d][u][1][1]};
                 o[d0 + d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, w[u]), o[d0 + d], 0, 0, 0);
+                o[d0 + d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, rest[u]), o[d0 + d], 0, 0, 0);
             }
     }
 }

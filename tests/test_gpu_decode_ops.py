@@ -456,6 +456,15 @@ def test_attention_values_that_are_not_finite_where_they_are_seen(pools, name):
 
 
 @pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_attention_of_a_channel_of_infinities(pools, name):
+    """Whatever parts a weight has, each is above zero: infinities of one sign stay what they are."""
+    kv = [1, 31, 700, 64]
+    c = Cache(name, kv, 16, 2, 64, seed=9)
+    c.to(c.v)[..., 0, 5], c.to(c.v)[..., 1, 60] = INF, -INF
+    run_attention(pools, name, kv, 6, 2, 64, cache=c, unseen=None, seed=9)
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
 @pytest.mark.parametrize("heads,dim", [(4, 64), (24, 128)])
 def test_attention_queries_and_keys_that_are_not_finite(pools, name, heads, dim):
     """A NaN of a query stays in its head, one of a key in the heads that read it."""
@@ -499,6 +508,20 @@ def test_attention_scores_of_minus_infinity(pools, name, heads, first, last):
 @pytest.mark.parametrize("scale", [-0.3, 1.0, 30.0, 1e-30])
 def test_attention_scales(pools, name, scale):
     run_attention(pools, name, [300, 40], 2, 2, 32, scale=scale)
+
+
+@pytest.mark.parametrize("heads,hk,dim", [(4, 2, 64), (8, 2, 128), (33, 1, 32), (2, 1, 72)])
+def test_attention_results_are_rounded_once(pools, heads, hk, dim):
+    """The weights' own error counts for less than 2^-14 in the sum of |p v|: in bf16 they are two parts, of which the second
+    (below 2^-7 of the weight) is off by half a step, 2^-8 of it.  The rest is the bound of fp32 and the result's rounding."""
+    kv = [3000, 1, 0, 513, 31, 1024]
+    c = Cache("bf16", kv, 16, hk, dim, seed=dim)
+    q = (torch.randn(len(kv), heads * dim, generator=gen(dim)) * 0.5).bfloat16()
+    got = run_attention(pools, "bf16", kv, heads, hk, dim, cache=c, q=q).view(len(kv), heads, dim)
+    k, v = (torch.where(t.isnan(), 0.0, t.float()) for t in c.host())  # (what is not seen holds NaNs)
+    want, bound = ref.paged_attention(q.float().view(len(kv), heads, dim), k, v, c.table, kv, 0, 0, 0.0)
+    spread, _ = ref.paged_attention(q.float().view(len(kv), heads, dim), k, v.abs(), c.table, kv, 0, 0, 0.0)
+    block_ops_util.assert_within(got, want, bound + 2.0 ** -14 * spread + 1.01 * 2.0 ** -8 * want.abs(), f"{heads}/{hk} heads of {dim}")
 
 
 @pytest.mark.parametrize("name", ["f32", "bf16"])
