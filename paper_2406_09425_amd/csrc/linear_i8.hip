@@ -628,42 +628,46 @@ static int plan_linear_i8(const sgprs_linear_i8_desc_t& d, int cus, bool direct,
     return best;
 }
 
-template <auto kernel> static int launch_sized(int lds, const LinearI8Args& a, int threads, hipStream_t stream)
+// By tiles of bm x bn outputs.  A launch has less than 2^32 threads: rows in bands.  (n is at most 2^20, so that a band has 127 row
+// tiles or more.)
+template <auto kernel> static int launch_sized(int lds, LinearI8Args a, int bm, int bn, int threads, hipStream_t stream)
 {
-    if ((long long)a.grid_m * a.grid_n * threads >= (1ll << 32)) return fail(SGPRS_ERR_UNSUPPORTED, "%d x %d outputs", a.m, a.n);
     static std::atomic<bool> raised{false};  // more than the default 64 KiB of dynamic LDS needs an opt-in per kernel
     if (lds > 65536 && !raised) {
         SGPRS_HIP(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
         raised = true;
     }
-    SGPRS_LAUNCH(kernel, dim3((unsigned)((long long)a.grid_m * a.grid_n)), threads, lds, stream, a);
-    SGPRS_HIP(hipGetLastError());
-    return SGPRS_OK;
-}
-
-static LinearI8Args tiled(LinearI8Args a, int bm, int bn)
-{
-    a.grid_m = (a.m - 1) / bm + 1;  // (m may be the largest int)
     a.grid_n = (a.n - 1) / bn + 1;
-    return a;
+    const long long band = ((1ll << 32) - 1) / threads / a.grid_n * bm, m = a.m;
+    for (long long done = 0; done < m; done += band) {
+        a.m = (int)std::min(m - done, band);
+        a.grid_m = (a.m - 1) / bm + 1;  // (m may be the largest int)
+        SGPRS_LAUNCH(kernel, dim3((unsigned)((long long)a.grid_m * a.grid_n)), threads, lds, stream, a);
+        SGPRS_HIP(hipGetLastError());
+        a.x += band * a.ldx;
+        a.y += band * a.ldy;
+        if (a.x_scales) a.x_scales += band;
+        if (a.residual) a.residual += band * a.ldr;
+    }
+    return SGPRS_OK;
 }
 
 template <int DT, int ACT, int BM, int BN, int NS> static int launch_tile(const LinearI8Args& a, hipStream_t stream)
 {
-    return launch_sized<linear_i8_tile_kernel<DT, ACT, BM, BN, NS>>(NS * (BM + BN) * 128, tiled(a, BM, BN), 256, stream);
+    return launch_sized<linear_i8_tile_kernel<DT, ACT, BM, BN, NS>>(NS * (BM + BN) * 128, a, BM, BN, 256, stream);
 }
 template <int DT, int ACT, int BM, int BN> static int launch_staged(const LinearI8Args& a, hipStream_t stream)
 {
-    return launch_sized<linear_i8_staged_kernel<DT, ACT, BM, BN>>(2 * (BM + BN) * 128, tiled(a, BM, BN), 256, stream);
+    return launch_sized<linear_i8_staged_kernel<DT, ACT, BM, BN>>(2 * (BM + BN) * 128, a, BM, BN, 256, stream);
 }
 template <int DT, int ACT, bool DIRECT, int TM, int TN, int NW, int NS> static int launch_ksplit(const LinearI8Args& a, hipStream_t stream)
 {
-    return launch_sized<linear_i8_ksplit_kernel<DT, ACT, TM, TN, NW, NS, DIRECT>>(NW * NS * (TM + TN) * 2048, tiled(a, 16 * TM, 16 * TN), NW * 64, stream);
+    return launch_sized<linear_i8_ksplit_kernel<DT, ACT, TM, TN, NW, NS, DIRECT>>(NW * NS * (TM + TN) * 2048, a, 16 * TM, 16 * TN, NW * 64, stream);
 }
 
 template <int DT, int ACT, bool DIRECT> static int launch_planned(const LinearI8Args& a, int kernel, hipStream_t stream)
 {
-    if (kernel == kShort) return launch_sized<linear_i8_short_kernel<DT, ACT>>(0, tiled(a, 64, 64), 256, stream);
+    if (kernel == kShort) return launch_sized<linear_i8_short_kernel<DT, ACT>>(0, a, 64, 64, 256, stream);
     if constexpr (DIRECT) {
         switch (kernel) {
         case kTile256: return launch_tile<DT, ACT, 256, 256, 2>(a, stream);

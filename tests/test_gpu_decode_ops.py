@@ -323,6 +323,36 @@ def test_rows_behind_four_gigabytes(pools):
     assert torch.equal(bits(y[:67 * 1000000].view(1000000, 67, 40)), bits(y[:67].expand(1000000, 67, 40).contiguous()))
 
 
+@pytest.mark.parametrize("n,k", [(1, 8), (8, 16)])
+def test_linear_of_more_tiles_than_a_launch_holds(pools, n, k):
+    """2^30 rows and a few: 2^24 tiles of 64 of them, 256 threads each, are 2^32 threads (repeated rows: what is before the
+    last ones is the same)."""
+    m, few, g = (1 << 30) + 5, 61, gen(k)
+    x, w = (torch.randint(-127, 128, (rows, k), generator=g, dtype=torch.int8) for rows in (few, n))
+    sx, res = torch.rand(few, generator=g), torch.randn(few, n, generator=g).bfloat16()
+
+    def repeated(t):
+        whole, full = torch.empty((m,) + t.shape[1:], dtype=t.dtype, device="cuda"), m // few
+        whole[:full * few].view((full,) + t.shape).copy_(t.cuda().expand((full,) + t.shape))
+        whole[full * few:] = t[:m - full * few].cuda()
+        return whole
+
+    X, SX, R, W, Y = repeated(x), repeated(sx), repeated(res), w.cuda(), torch.zeros(m, n, dtype=torch.bfloat16, device="cuda")
+    pool = pools()
+    torch.cuda.synchronize()
+    S.sgprs_linear_i8(S.LinearI8Desc(m=m, n=n, k=k, dtype=1), ptr(X), ptr(SX), ptr(W), None, None, ptr(R), ptr(Y), None, 0, pool, 0)
+    pool.sync()
+    want, bound = ref.linear_i8(x, sx, w, None, None, res, 0, 0, torch.bfloat16)
+    rows = torch.arange(m - 400, m)  # on both sides of 2^30 - 64
+    block_ops_util.assert_within(Y[m - 400:], want[rows % few], bound[rows % few], "last rows")
+    block_ops_util.assert_within(Y[:few], want, bound, "first rows")
+    blocks = Y[:m // few * few].view(-1, few, n).view(torch.int16)
+    for part in blocks.split(1 << 22):
+        assert bool((part == blocks[0]).all())
+    del X, SX, R, Y, blocks, part
+    torch.cuda.empty_cache()
+
+
 # ---- paged cache ---------------------------------------------------------------------------------
 class Cache:
     """Caches of n_pages pages; layout: the order of the page's positions and heads."""
