@@ -13,6 +13,10 @@ int check_linear_i8(const sgprs_linear_i8_desc_t* d, sgprs_linear_i8_desc_t* ful
 int check_paged_append(const sgprs_paged_append_desc_t* d, sgprs_paged_append_desc_t* full);
 int check_paged_attention(const sgprs_paged_attention_desc_t* d, sgprs_paged_attention_desc_t* full);
 
+// Kernels of the 8-bit product, and the one that it is planned by on `cus` CUs.  direct: aligned rows of whole 16-byte chunks.
+enum LinearI8Kernel { kTile256, kTile128, kTile64, kDeep128, kDeep64, kStaged128, kStaged64, kStaged32, kSplit16x16, kSplit32x16, kSplit64x16, kSplit32x32, kSplit64x32, kSplit32x64, kSplit64x64, kShort };
+int plan_linear_i8(const sgprs_linear_i8_desc_t& d, int cus, bool direct, bool residual);
+
 size_t linear_i8_workspace_bytes(const sgprs_linear_i8_desc_t& d, int cus);
 size_t paged_attention_workspace_bytes(const sgprs_paged_attention_desc_t& d, int cus);
 

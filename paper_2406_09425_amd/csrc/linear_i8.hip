@@ -581,8 +581,6 @@ template <int DT, int ACT, int TM, int TN, int NW, int NS, bool DIRECT> __global
 }
 
 // ---- plans -------------------------------------------------------------------------------------
-enum LinearI8Kernel { kTile256, kTile128, kTile64, kDeep128, kDeep64, kStaged128, kStaged64, kStaged32, kSplit16x16, kSplit32x16, kSplit64x16, kSplit32x32, kSplit64x32, kSplit32x64, kSplit64x64, kShort };
-
 // Integers are summed exactly in any order, but no kernel splits k over workgroups: with a join in a second launch 128x4096
 // -> 4096 took 17 us, where the wavefronts of a workgroup split it in 8.5.
 size_t linear_i8_workspace_bytes(const sgprs_linear_i8_desc_t&, int) { return 0; }
@@ -592,7 +590,7 @@ size_t linear_i8_workspace_bytes(const sgprs_linear_i8_desc_t&, int) { return 0;
 // 256 / 128 / 64 square tiles, 64x64 / 32x32 / 16x16 with k split: 16384x4096 -> 4096 237 / 283 / 430 us, 12544x512 -> 2048
 // 33 / 30 / 39, 2048x1024 -> 1024 19 / 9.5 / 7.1 / 10.8, 256x4096 -> 4096 43 / 23 (17 with four k-tiles) / 18 (10.6) / 10.6 / 22, 64x4096 ->
 // 4096 42 / 23 / 17 / 9.9 / 7.3 / 17, 1x4096 -> 4096 39 / 21 / 16 / 8.8 / 6.2 / 5.7.
-static int plan_linear_i8(const sgprs_linear_i8_desc_t& d, int cus, bool direct, bool residual)
+int plan_linear_i8(const sgprs_linear_i8_desc_t& d, int cus, bool direct, bool residual)
 {
     if (d.k < 16) return kShort;
     const double kt = (d.k + 127) / 128;

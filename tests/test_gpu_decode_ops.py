@@ -8,6 +8,7 @@ import torch
 import block_ops_util
 import decode_ops_util as ref
 import paper_2406_09425_amd as S
+from linear_i8_shapes import SHAPES
 from test_gpu_block_ops import CUS, DT, Rows, gen, pools, ptr  # noqa: F401  (pools is a fixture)
 
 pytestmark = pytest.mark.gpu
@@ -254,6 +255,14 @@ def test_linear_shapes(pools, name, shape):
 def test_linear_tiles_of_every_size(pools, name, shape, res):
     m, n, k = shape
     run_linear(pools, name, m, n, k, act=int(res), bias=not res, res=res, seed=m)
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("kernel,shape", SHAPES, ids=lambda s: s if isinstance(s, str) else "x".join(map(str, s)))
+def test_linear_by_every_kernel(pools, name, kernel, shape):
+    m, n, k = shape
+    for res in (False, True):
+        run_linear(pools, name, m, n, k, act=3 if res else 0, bias=not res, res=res, first=int(res), seed=n)
 
 
 @pytest.mark.parametrize("shape", [(1, 100, 512), (20, 64, 300), (40, 200, 130), (300, 130, 96), (1000, 1500, 200), (3000, 2100, 256)], ids=lambda s: "x".join(map(str, s)))
