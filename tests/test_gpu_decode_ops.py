@@ -579,6 +579,29 @@ def test_attention_of_many_sequences(pools, name, n):
 
 
 @pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [300, 2000])
+def test_attention_of_tables_for_long_sequences(pools, name, n):
+    """Room for 2^30 positions a sequence: the costs of all of them fit 31 bits in units of 8 (n 300) or 32 (2000) tiles only.
+    Sequences of a fraction of a unit, whole ones and one that several workgroups share read the same page."""
+    dim, heads, tdt = 8, 2, DT[name][1]
+    kv = torch.randint(0, 40, (n,), generator=gen(n)).tolist()
+    for s, length in ((0, 0), (7, 255), (8, 256), (9, 257), (10, 1024), (11, 1025), (n // 2, 60001), (n - 2, 5000), (n - 1, 300)):
+        kv[s] = length
+    k, v = (torch.randn(1, max(kv), 1, dim, generator=gen(i)).to(tdt) for i in (1, 2))
+    q = (torch.randn(n, heads * dim, generator=gen(3)) * 1.5).to(tdt)
+    d = S.PagedAttentionDesc(n_seqs=n, heads=heads, kv_heads=1, head_dim=dim, dtype=DT[name][0], n_pages=1, page_size=1 << 30, table_width=1)
+    need = S.sgprs_paged_attention_workspace(d, CUS)
+    gk, gv, gq, lens, table = k.cuda(), v.cuda(), q.cuda(), torch.tensor(kv, dtype=torch.int32).cuda(), torch.zeros(n, 1, dtype=torch.int32, device="cuda")
+    o, ws = torch.full_like(gq, NAN), torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    S.sgprs_paged_attention(d, ptr(gq), ptr(gk), ptr(gv), ptr(table), ptr(lens), ptr(o), ptr(ws), need, pools(), 0)
+    pools().sync()
+    want, bound = ref.paged_attention(q.view(n, heads, dim), k, v, table.cpu(), kv, 0, 0, 0.0)
+    block_ops_util.assert_within(o.view(n, heads, dim), want, bound, f"{name} {n}")
+    assert bool((ws[need:] == 255).all())
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
 @pytest.mark.parametrize("heads,hk,dim", [(2, 1, 32), (3, 1, 128), (5, 1, 64), (8, 1, 24), (14, 2, 128), (16, 2, 96), (9, 1, 32), (16, 1, 128)])
 def test_attention_of_few_heads_of_a_key_head(pools, name, heads, hk, dim):
     run_attention(pools, name, [333, 64, 1, 0, 130], heads, hk, dim, seed=heads + dim)
@@ -646,6 +669,30 @@ def test_attention_lengths_and_tables_outside_their_range(pools, name):
     S.sgprs_paged_attention(d, ptr(q), ptr(c.gk), ptr(c.gv), ptr(c.gtable), ptr(c.glens), ptr(o), ptr(ws), need, pools(), 0)
     pools().sync()
     assert bool(torch.isfinite(o).all()) and bool((o[1] == 0).all()) and good is not None
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_attention_of_other_sequences_beside_entries_of_no_page(pools, name):
+    """Sequences whose entries are fine give the bits that they give beside good ones, with and without a split."""
+    kv = [64, 0, 48, 700, 33, 5000]
+    c = Cache(name, kv, 16, 2, 64, seed=3).to_gpu()
+    q, o = (torch.randn(len(kv), 256, generator=gen(i)).to(DT[name][1]).cuda() for i in (1, 2))
+    d = S.PagedAttentionDesc(heads=4, **c.dims)
+    need = S.sgprs_paged_attention_workspace(d, CUS)
+    ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+
+    def call():
+        torch.cuda.synchronize()
+        S.sgprs_paged_attention(d, ptr(q), ptr(c.gk), ptr(c.gv), ptr(c.gtable), ptr(c.glens), ptr(o), ptr(ws), need, pools(), 0)
+        pools().sync()
+        return o.cpu()
+
+    good = call()
+    c.gtable[0, 1], c.gtable[0, 2], c.gtable[2, 0], c.gtable[3, 40] = -7, 2 ** 31 - 1, c.n_pages, -2 ** 31
+    got = call()
+    for s in (1, 4, 5):
+        assert torch.equal(bits(got[s]), bits(good[s])), s
+    assert bool(torch.isfinite(got).all())
 
 
 # ---- new keys and values -------------------------------------------------------------------------
