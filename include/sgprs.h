@@ -426,7 +426,8 @@ int sgprs_linear_i8_workspace(const sgprs_linear_i8_desc_t *d, int partition_cus
 /* x int8 [m][k], w int8 [n][k] (any values, -128 too), residual NULL or [m][n],
  * y [m][n] DEVICE; x_scales NULL (1) or fp32[m], w_scales NULL (1) or fp32[n],
  * bias NULL or fp32[n] DEVICE.  y may be the residual (same pointer and stride).
- * Fastest where x, w and their strides are multiples of 16 bytes. */
+ * Fastest where x, w, their strides and k are multiples of 16 bytes; zeros behind k in x and
+ * w change no sum, so rows that are padded with them may count them into k. */
 int sgprs_linear_i8(const sgprs_linear_i8_desc_t *d, const int8_t *x, const float *x_scales,
                     const int8_t *w, const float *w_scales, const float *bias, const void *residual,
                     void *y, void *workspace, size_t workspace_bytes, sgprs_pool_t *pool,

@@ -254,8 +254,8 @@ template <int N, int M> __device__ __forceinline__ void settle(i32x4_t (&acc)[N]
 // at once while the next k-tile's first fragments are read and the one after that is requested into the buffer just left.
 // NS k-tiles in LDS: four where few tiles leave it free, 1024x4096 -> 4096 by 128x128 tiles 26 -> 22 us, 256x4096 -> 4096 by
 // 64x64 18 -> 10.6; where several workgroups share a CU two are faster (2048x4096 -> 4096 35 for 42).
-// 16384x4096 -> 4096 in 240 to 255 us, by card (2.2 to 2.3 PFLOP/s; the library's product of integers alone 259): bound by
-// the MFMAs and the clock under them.  32x32x32 MFMAs took 255 for 237, a ring of four half k-tiles 258 for 255.
+// 16384x4096 -> 4096 in 238 to 262 us, by card (2.1 to 2.3 PFLOP/s; the library's product of integers alone 259 to 270): bound
+// by the MFMAs and the clock under them (of 30 launches without a pause the first five take 256 to 265, the others 271 to 292).  32x32x32 MFMAs took 255 for 237, a ring of four half k-tiles 258 for 255.
 template <int DT, int ACT, int BM, int BN, int NS> __global__ __launch_bounds__(256, BM * BN >= 256 * 128 ? 1 : 2) void linear_i8_tile_kernel(const LinearI8Args a)
 {
 #if __HIP_DEVICE_COMPILE__
@@ -361,9 +361,10 @@ template <int DT, int ACT, int BM, int BN, int NS> __global__ __launch_bounds__(
 // BM x BN outputs, 2 x 2 wavefronts; the next k-tile is on its way to registers while this one, in one of two LDS buffers, is
 // multiplied.  k >= 16: loads have no branch; a chunk that reaches past the end of its row is taken from the row's
 // last 16 bytes and shifted when it is stored, rows past the end repeat the last one.
-// Few tiles are 32 rows high: 700x700 -> 701 in bf16 5.9 us, by 64x64 tiles 7.3, 1000x1000 -> 500 7.2 for 8.2.
-// 3137x517 -> 509 in fp32 in 8 us, with a residual 9.1 (by 64x64 tiles 9.8): few k-tiles, each a round trip to memory.  Two
-// k-tiles on their way took 8.6 for 7.5, residuals and scales asked for before the k loop 8.5 for 7.9.
+// Few tiles are 32 rows high: 700x700 -> 701 in bf16 5.4 us, by 64x64 tiles 6.1, 1500x300 -> 300 in fp32 with a residual 4.8 for
+// 6.0, 3137x250 -> 509 6.6 for 7.6, without a residual 6.4 for 6.2.
+// 3137x517 -> 509 in fp32 in 8 us, with a residual 9.1 (by 64x64 tiles 9.8): few k-tiles, each a round trip to memory.  Of
+// 64x64 tiles two k-tiles on their way took 8.6 for 7.5; residuals and scales asked for before the k loop 8.5 for 7.9.
 template <int DT, int ACT, int BM, int BN> __global__ __launch_bounds__(256, 2) void linear_i8_staged_kernel(const LinearI8Args a)
 {
 #if __HIP_DEVICE_COMPILE__

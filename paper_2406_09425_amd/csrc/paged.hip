@@ -12,7 +12,7 @@
 // Measured, both launches, 256 CUs: 16 caches of 1 to 32768 tokens, 32/8 heads of 128 in bf16, 60 us (55 and 5; 265 MB, 4.5
 // TB/s); 16 of 4096, 8 heads of 128 in fp32, 102 (5.3 TB/s).  With a run for each wavefront instead of each workgroup 16 equal
 // caches took 69 for 61: four times the partial sums.  Few short caches are a chain of latencies (lengths, table, keys, the
-// join's launch): three of up to 700 in 8.6 us, one of 2048 in 10.
+// join's launch): three of up to 700 in 8.7 us, one of 2048 in 11.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -98,7 +98,7 @@ struct Runs {
 //   values: a read brings PK keys, CHUNKS lanes each; the weights reach the lanes as row operands, where the instruction
 //           hands those of one block in each group of blocks to all of the group.  Lane l ends up with channels
 //           4 (l % CHUNKS) + e of all four queries, summed over every PK-th key.
-// 16 caches of 4096, 8/8 heads of 128: 111 us, by 32 x 32 x 2 MFMAs 151.
+// 16 caches of 4096, 8/8 heads of 128, when this was written: 111 us, by 32 x 32 x 2 MFMAs 151 (now 102).
 template <int HD, int SETS> struct RunningNarrow {
     typedef KvTile<SGPRS_F32, HD> Tile;
     static constexpr int CHUNKS = Tile::CHUNKS, PK = 64 / CHUNKS, GROUP_LOG2 = CHUNKS == 32 ? 3 : CHUNKS == 16 ? 2 : 1;  // blocks of a group
@@ -246,6 +246,8 @@ struct Segment {
 #endif
 
 // SETS: of four heads of a key head, in fp32; 0: up to 32 heads.
+// No vector register is spilled; of the scalars (some 50 dwords of arguments, segments, masks of padded chunks) 58 to 183 live in
+// lanes of vector registers.  Channels 65 to 96 in fp32 take rows of 128 in LDS (138624 bytes, one workgroup of a CU).
 template <int DT, int HD, int SETS> __global__ __launch_bounds__(256, (PagedShape<DT, HD>::PER_CU)) void paged_attention_kernel(const PagedArgs a)
 {
 #if __HIP_DEVICE_COMPILE__
